@@ -351,6 +351,126 @@ int httm_selftest_tensor_core(const void* q, const void* k, const void* v, float
  * the context was used on.  NULL is accepted. */
 int httm_destroy(httm_ctx* ctx);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * A kept scene: what stands in front of the attention of a layer, and what lets later tokens attend to earlier ones.
+ *
+ *   httm_norm_rotate       norms of queries and keys for each head and their rotation by position, in one pass
+ *   httm_cache_append      new keys (normed and rotated on the way) and values into the pages of a cache
+ *   httm_cache_attention   attention of a batch of sequences: all of them see one shared prefix (the encoded scene, a
+ *                          common document), and each its own keys behind it
+ *
+ * They take bf16 or fp16 tensors [heads][tokens][head_dim] under the rules of httm_tensor above (16-byte aligned,
+ * strides multiples of 8 elements), work on any stream, and need no httm_ctx.  Where a call fails, httm_last_error(NULL)
+ * gives the reason (per thread).  A handle is not thread-safe and the calls that use it have to be ordered (one stream,
+ * or events between streams); separate handles are independent.
+ */
+enum { HTTM_BF16 = 0, HTTM_FP16 = 1 };
+enum { HTTM_NORM_NONE = 0, HTTM_NORM_RMS = 1, HTTM_NORM_LAYER = 2 };
+
+typedef struct httm_rotary httm_rotary; /* opaque: the rotation's table and the kind of norm */
+
+typedef struct {
+    int32_t device;
+    int32_t head_dim;      /* 32, 64, 128 or 256                                                             */
+    int32_t norm;          /* HTTM_NORM_*                                                                    */
+    int32_t rotated_dim;   /* the first rotated_dim channels rotate; a multiple of 8 * axes, 0: no rotation  */
+    int32_t axes;          /* 1, or 2: the first half of them by the row, the second by the column           */
+    int32_t interleaved;   /* pairs are channels (2i, 2i + 1) of an axis instead of (i, i + d/2)             */
+    int32_t n_positions;   /* positions 0 .. n_positions - 1                                                 */
+    double eps;
+    double base;           /* angle of pair i per position: base^(-2i/d), d = rotated_dim / axes             */
+    const double* frequencies; /* host, [d / 2]: these angles instead, or NULL                               */
+} httm_rotary_config;
+
+/* cos and sin of every position are computed here (64 bits, kept in 32).  Errors: INVALID_ARG, UNSUPPORTED, NOMEM, CUDA. */
+int httm_rotary_create(const httm_rotary_config* config, httm_rotary** out);
+int httm_rotary_destroy(httm_rotary* rotary);
+/* Waits for the device.  *status: 0, or the first device-side error of the calls made with this handle (then also the
+ * return value): a position outside the table, whose rows come out as NaN. */
+int httm_rotary_status(httm_rotary* rotary, int64_t* status);
+
+typedef struct {
+    httm_tensor x;       /* read                                                                             */
+    httm_tensor y;       /* written; x itself (in place) or a tensor without overlap                         */
+    int32_t heads;
+    const float* weight; /* device, [head_dim], or NULL (1)                                                  */
+    const float* bias;   /* device, [head_dim], or NULL (0)                                                  */
+} httm_rows;
+
+/* y = rotate(norm(x) * weight + bias) for every row (head, token), positions [n_tokens][axes] on the device.  q or k may be NULL.
+ * Norm and rotation are computed in 32 bits and rounded once. */
+int httm_norm_rotate(httm_rotary* rotary, int32_t dtype, int64_t n_tokens, const int32_t* positions, const httm_rows* q,
+                     const httm_rows* k, void* cuda_stream);
+
+typedef struct {
+    httm_tensor x, dy;   /* read: the input of the forward pass, the gradient of its output                  */
+    httm_tensor dx;      /* written; dy or x itself (in place) or a tensor without overlap                   */
+    int32_t heads;
+    const float* weight; /* as in the forward pass                                                           */
+    float* dweight;      /* written: [head_dim], or NULL                                                     */
+    float* dbias;        /* written: [head_dim], or NULL                                                     */
+} httm_rows_grad;
+
+/* The gradients of httm_norm_rotate.  Those of weight and bias are sums over all rows, in 32 bits and in an order that depends on
+ * the sizes alone: the same call gives the same bits. */
+int httm_norm_rotate_backward(httm_rotary* rotary, int32_t dtype, int64_t n_tokens, const int32_t* positions,
+                              const httm_rows_grad* q, const httm_rows_grad* k, void* cuda_stream);
+
+typedef struct httm_batch httm_batch; /* opaque: the sequences of one step, their pages, the plan of their attention */
+
+typedef struct {
+    int32_t device;
+    int32_t heads, kv_heads; /* heads a multiple of kv_heads, at most 64 query heads to a key head                 */
+    int32_t head_dim;        /* 64 or 128                                                                         */
+    int32_t page_size;       /* tokens of a page: 16, 32, 64, 128 or 256                                          */
+    int32_t causal;          /* 1: of its own keys a query sees those up to its own place; 0: all of them         */
+    int64_t n_pages;         /* pages of the caches it is used with (n_pages * page_size < 2^31)                  */
+} httm_batch_config;
+
+int httm_batch_create(const httm_batch_config* config, httm_batch** out);
+int httm_batch_destroy(httm_batch* batch);
+/* As httm_rotary_status: a bounded wait that ran out. */
+int httm_batch_status(httm_batch* batch, int64_t* status);
+
+/*
+ * The sequences of the next calls.  All arrays are HOST memory and are read before the call returns.
+ *   lengths[i]   keys of sequence i in the cache, the new ones of this step included
+ *   queries[i]   its query tokens, which stand one behind the other in q, k, v and out: sequence 0 first
+ *   tables       pages of sequence i at tables + i * table_stride, as many as its length takes; key j is in slot
+ *                j % page_size of page j / page_size
+ *   prefix_pages, prefix_length   the keys that every sequence sees in front of its own
+ * A plan of the attention is made here, so that a batch serves all layers of a step.  It is uploaded on `cuda_stream`; memory
+ * grows here when a batch is larger than all before it, nothing is allocated in the calls below.  Errors: INVALID_ARG (a page
+ * that does not exist, a negative length), UNSUPPORTED, NOMEM, CUDA; the batch is then empty.
+ */
+int httm_batch_set(httm_batch* batch, int32_t n_sequences, const int32_t* lengths, const int32_t* queries, const int32_t* tables,
+                   int64_t table_stride, const int32_t* prefix_pages, int32_t prefix_length, void* cuda_stream);
+
+typedef struct {
+    void* ptr;            /* device pointer, 16-byte aligned: element [page][head][slot][channel]                 */
+    int64_t stride_page;  /* elements; all strides are multiples of 8, channels contiguous                        */
+    int64_t stride_head;
+    int64_t stride_slot;
+} httm_pages;
+
+/*
+ * The tokens of the batch into its pages: the queries[i] tokens of sequence i go to its last queries[i] places.  k and v are
+ * [kv_heads][tokens][head_dim].  With `rotary` (may be NULL) keys are normed and rotated on the way as in httm_norm_rotate, by `positions`
+ * ([tokens][axes], device) or, where that is NULL and the handle has one axis, by the token's place behind the prefix.
+ * INVALID_ARG where a sequence has fewer keys than queries, or two tokens would go to the same place (a page that two sequences write,
+ * or a page of the prefix).
+ */
+int httm_cache_append(httm_batch* batch, int32_t dtype, httm_pages k_pages, httm_pages v_pages, httm_tensor k, httm_tensor v,
+                      httm_rotary* rotary, const int32_t* positions, const float* k_weight, const float* k_bias, void* cuda_stream);
+
+/*
+ * out[h][t] = softmax(scale * q[h][t] . K^T) V over the prefix and the keys of t's own sequence (up to its own place if causal: token
+ * i of n sees keys j <= length - n + i).  A query that sees no key gets zeros.  Keys and values outside a sequence's length are
+ * not touched by any sum, whatever the pages hold there.  Scores, maxima and sums are kept in 32 bits.
+ */
+int httm_cache_attention(httm_batch* batch, int32_t dtype, httm_pages k_pages, httm_pages v_pages, httm_tensor q, httm_tensor out,
+                         double scale, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,273 @@
+// Batches over a paged cache: which tokens go where, and how the attention of a step is dealt to the SMs.
+//
+// The plan.  A ROW TILE is a run of tokens (all heads of the group that share a key head) and the keys they see: the prefix, the own keys of a
+// sequence, or both one behind the other.  Sequences with few rows leave the prefix to row tiles that span sequences, so that it is read once for all of
+// them, and look at their own keys in tiles of their own; sequences with many rows see both in one pass.  A JOB is a row tile, a key head and a
+// run of its key tiles.  Jobs are dealt so that every CTA has the same number of key tiles to walk: whole row tiles as long as they fit, in order,
+// each to the CTA that has least so far (CTAs at work at the same time then read neighbouring keys), and what is left is cut where
+// a CTA is full.  A row whose keys were cut, or lie in two row tiles, leaves partial results that a last kernel adds up; others are written by their job.
+#include <algorithm>
+#include <cmath>
+#include <exception>
+#include <new>
+#include <string>
+#include <utility>
+
+#include "httm_batch_plan.h"
+#include "httm_cache.h"
+#include "httm_internal.h"
+
+using namespace httm;
+
+struct httm_batch {
+    httm_batch_config cfg{};
+    int32_t sm_count = 148;
+    BatchPlan plan;
+    BatchLayout at;                  // where the parts of the plan lie in `data`
+    bool set = false;
+    unsigned char* data = nullptr;   // device copy of the plan
+    unsigned char* staged = nullptr; // pinned
+    size_t data_bytes = 0, staged_bytes = 0;
+    float* partial = nullptr;
+    size_t partial_floats = 0;
+    int32_t* status = nullptr;
+    cudaEvent_t uploaded = nullptr;
+    ~httm_batch() {
+        for (void* p : {(void*)data, (void*)partial, (void*)status})
+            if (p) cudaFree(p);
+        if (staged) cudaFreeHost(staged);
+        if (uploaded) cudaEventDestroy(uploaded);
+    }
+};
+
+namespace {
+
+int cuda_result(cudaError_t e, const char* what) {
+    if (e == cudaSuccess) return HTTM_OK;
+    cudaGetLastError();
+    return global_fail(e == cudaErrorMemoryAllocation ? HTTM_ERR_NOMEM : HTTM_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+// Room for `bytes`, half as much again so that a growing batch does not come here at every step.
+template <typename T>
+int grow(T** p, size_t* have, size_t need, bool pinned) {
+    if (need <= *have) return HTTM_OK;
+    const size_t n = need + need / 2 + 256;
+    if (*p) {
+        if (pinned)
+            cudaFreeHost(*p);
+        else
+            cudaFree(*p);   // (waits for the kernels that use it)
+    }
+    *p = nullptr;
+    *have = 0;
+    const cudaError_t e = pinned ? cudaMallocHost(reinterpret_cast<void**>(p), n * sizeof(T)) : cudaMalloc(reinterpret_cast<void**>(p), n * sizeof(T));
+    if (e != cudaSuccess) {
+        *p = nullptr;
+        return cuda_result(e, "batch");
+    }
+    *have = n;
+    return HTTM_OK;
+}
+
+int check_pages(const httm_pages& t, const httm_batch_config& c, const char* name) {
+    if (!t.ptr) return global_fail(HTTM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if (((uintptr_t)t.ptr & 15u) != 0) return global_fail(HTTM_ERR_ALIGNMENT, "%s: pointer is not 16-byte aligned", name);
+    if (t.stride_page % 8 != 0 || t.stride_head % 8 != 0 || t.stride_slot % 8 != 0)
+        return global_fail(HTTM_ERR_ALIGNMENT, "%s: strides must be multiples of 8 elements", name);
+    // rows must not overlap one another: from the smallest stride to the largest, each steps over all that the ones before it reach
+    std::pair<int64_t, int64_t> dims[3] = {{t.stride_slot, c.page_size}, {t.stride_head, c.kv_heads}, {t.stride_page, c.n_pages}};
+    std::sort(dims, dims + 3);
+    int64_t reach = c.head_dim;
+    for (const auto& d : dims) {
+        if (d.second == 1) continue;
+        if (d.first < reach) return global_fail(HTTM_ERR_INVALID_ARG, "%s: strides must be >= head_dim, and rows must not overlap", name);
+        reach += d.first * (d.second - 1);
+    }
+    return HTTM_OK;
+}
+int check_common(httm_batch* b, int32_t dtype, const char* what) {
+    if (!b) return global_fail(HTTM_ERR_INVALID_ARG, "%s: null batch", what);
+    if (dtype != HTTM_BF16 && dtype != HTTM_FP16) return global_fail(HTTM_ERR_INVALID_ARG, "%s: dtype must be HTTM_BF16 or HTTM_FP16", what);
+    if (!b->set) return global_fail(HTTM_ERR_INVALID_ARG, "%s: the batch has not been set", what);
+    return HTTM_OK;
+}
+
+template <typename T>
+const T* part_of(const httm_batch* b, size_t offset) {
+    return reinterpret_cast<const T*>(b->data + offset);
+}
+
+}  // namespace
+
+extern "C" {
+
+int httm_batch_create(const httm_batch_config* config, httm_batch** out) {
+    if (out) *out = nullptr;
+    if (!config || !out) return global_fail(HTTM_ERR_INVALID_ARG, "batch: null argument");
+    const httm_batch_config& c = *config;
+    if (c.heads < 1 || c.kv_heads < 1 || c.heads % c.kv_heads != 0 || c.heads > 65535)
+        return global_fail(HTTM_ERR_INVALID_ARG, "batch: heads must be a positive multiple of kv_heads");
+    if (c.heads / c.kv_heads > 64) return global_fail(HTTM_ERR_UNSUPPORTED, "batch: at most 64 query heads to a key head");
+    if (c.head_dim != 64 && c.head_dim != 128) return global_fail(HTTM_ERR_UNSUPPORTED, "batch: head_dim must be 64 or 128");
+    if (c.page_size != 16 && c.page_size != 32 && c.page_size != 64 && c.page_size != 128 && c.page_size != 256)
+        return global_fail(HTTM_ERR_UNSUPPORTED, "batch: page_size must be 16, 32, 64, 128 or 256");
+    if (c.causal != 0 && c.causal != 1) return global_fail(HTTM_ERR_INVALID_ARG, "batch: causal must be 0 or 1");
+    if (c.n_pages < 1 || c.n_pages > ((1ll << 31) - 1) / c.page_size) return global_fail(HTTM_ERR_INVALID_ARG, "batch: number of pages out of range");
+    int devices = 0;
+    if (cudaGetDeviceCount(&devices) != cudaSuccess) cudaGetLastError(), devices = 0;
+    if (c.device < 0 || c.device >= devices) return global_fail(HTTM_ERR_INVALID_ARG, "batch: no such device");
+    OnDevice guard(c.device);
+    if (!guard.ok) return global_fail(HTTM_ERR_CUDA, "batch: cudaSetDevice failed");
+    httm_batch* b = new (std::nothrow) httm_batch;
+    if (!b) return global_fail(HTTM_ERR_NOMEM, "batch: out of host memory");
+    b->cfg = c;
+    cudaDeviceGetAttribute(&b->sm_count, cudaDevAttrMultiProcessorCount, c.device);
+    int rc = cuda_result(cudaMalloc(reinterpret_cast<void**>(&b->status), sizeof(int32_t)), "batch");
+    if (!rc) rc = cuda_result(cudaMemset(b->status, 0, sizeof(int32_t)), "batch");
+    if (!rc) rc = cuda_result(cudaEventCreateWithFlags(&b->uploaded, cudaEventDisableTiming), "batch");
+    if (!rc) rc = cuda_result(configure_cache_attention(), "batch");
+    if (!rc) rc = cuda_result(cudaDeviceSynchronize(), "batch");
+    if (rc) {
+        delete b;
+        return rc;
+    }
+    *out = b;
+    return HTTM_OK;
+}
+
+int httm_batch_destroy(httm_batch* b) {
+    if (!b) return HTTM_OK;
+    OnDevice guard(b->cfg.device);
+    delete b;
+    return HTTM_OK;
+}
+
+int httm_batch_status(httm_batch* b, int64_t* status) {
+    if (!b || !status) return global_fail(HTTM_ERR_INVALID_ARG, "batch: null argument");
+    OnDevice guard(b->cfg.device);
+    if (!guard.ok) return global_fail(HTTM_ERR_CUDA, "batch: cudaSetDevice failed");
+    int32_t s = 0;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpy(&s, b->status, sizeof s, cudaMemcpyDeviceToHost);
+    if (int rc = cuda_result(e, "batch status")) return rc;
+    *status = s;
+    if (s == kDevOk) return HTTM_OK;
+    return s == kDevBadIndex ? global_fail(HTTM_ERR_CUDA, "a position was outside the rotation's table")
+                             : global_fail(HTTM_ERR_TIMEOUT, "device status word = %d", (int)s);
+}
+
+int httm_batch_set(httm_batch* b, int32_t n_sequences, const int32_t* lengths, const int32_t* queries, const int32_t* tables, int64_t table_stride,
+                   const int32_t* prefix_pages, int32_t prefix_length, void* cuda_stream) {
+    if (!b) return global_fail(HTTM_ERR_INVALID_ARG, "batch_set: null batch");
+    b->set = false;
+    try {
+        std::string why;
+        const BatchInput in{n_sequences, lengths, queries, tables, table_stride, prefix_pages, prefix_length};
+        if (int rc = check_batch(b->cfg, in, &why)) return global_fail(rc, "batch_set: %s", why.c_str());
+        make_batch_plan(b->cfg, in, b->sm_count, &b->plan);
+        OnDevice guard(b->cfg.device);
+        if (!guard.ok) return global_fail(HTTM_ERR_CUDA, "batch_set: cudaSetDevice failed");
+        b->at = BatchLayout(b->plan);
+        if (int rc = cuda_result(cudaEventSynchronize(b->uploaded), "batch_set")) return rc;   // the last upload has left the staging buffer
+        if (int rc = grow(&b->staged, &b->staged_bytes, b->at.bytes, true)) return rc;
+        if (int rc = grow(&b->data, &b->data_bytes, b->at.bytes, false)) return rc;
+        if (int rc = grow(&b->partial, &b->partial_floats, (size_t)b->plan.part_units * kPartUnit * (b->cfg.head_dim + 2), false)) return rc;
+        b->at.write(b->plan, b->staged);
+        cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+        if (int rc = cuda_result(cudaMemcpyAsync(b->data, b->staged, b->at.bytes, cudaMemcpyHostToDevice, stream), "batch_set: upload")) return rc;
+        if (int rc = cuda_result(cudaEventRecord(b->uploaded, stream), "batch_set")) return rc;
+        b->set = true;
+        return HTTM_OK;
+    } catch (const std::exception&) {   // vectors and strings
+        return global_fail(HTTM_ERR_NOMEM, "batch_set: out of host memory");
+    }
+}
+
+int httm_cache_append(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_pages v_pages, httm_tensor k, httm_tensor v, httm_rotary* rotary,
+                      const int32_t* positions, const float* k_weight, const float* k_bias, void* cuda_stream) {
+    if (int rc = check_common(b, dtype, "append")) return rc;
+    const httm_batch_config& c = b->cfg;
+    const BatchPlan& p = b->plan;
+    if (!p.can_append) return global_fail(HTTM_ERR_INVALID_ARG, "append: a sequence has fewer keys than query tokens");
+    if (p.same_place) return global_fail(HTTM_ERR_INVALID_ARG, "append: two tokens would go to the same page of two sequences, or to a page of the prefix");
+    int rc = check_pages(k_pages, c, "append: k_pages");
+    if (!rc) rc = check_pages(v_pages, c, "append: v_pages");
+    if (!rc && p.n_tokens > 0) rc = check_rows_layout(k, c.kv_heads, p.n_tokens, c.head_dim, false, "append: k");
+    if (!rc && p.n_tokens > 0) rc = check_rows_layout(v, c.kv_heads, p.n_tokens, c.head_dim, false, "append: v");
+    if (rc) return rc;
+    RotaryView rot{};
+    if (rotary) {
+        rotary_view(rotary, &rot);
+        if (rot.head_dim != c.head_dim || rot.device != c.device) return global_fail(HTTM_ERR_INVALID_ARG, "append: the rotary handle is for another head_dim or device");
+        if (rot.norm == HTTM_NORM_NONE && (k_weight || k_bias)) return global_fail(HTTM_ERR_INVALID_ARG, "append: a weight or bias without a norm");
+        if ((((uintptr_t)k_weight | (uintptr_t)k_bias | (uintptr_t)positions) & 3u) != 0) return global_fail(HTTM_ERR_ALIGNMENT, "append: not aligned");
+        if (rot.table.rotated_dim > 0 && !positions) {
+            if (rot.table.axes != 1) return global_fail(HTTM_ERR_INVALID_ARG, "append: positions are missing");
+            if (p.last_position >= rot.table.n_positions) return global_fail(HTTM_ERR_INVALID_ARG, "append: a token's place is outside the rotation's table");
+        }
+    } else if (positions || k_weight || k_bias) {
+        return global_fail(HTTM_ERR_INVALID_ARG, "append: positions or weights without a rotary handle");
+    }
+    if (p.n_tokens == 0) return HTTM_OK;
+    OnDevice guard(c.device);
+    if (!guard.ok) return global_fail(HTTM_ERR_CUDA, "append: cudaSetDevice failed");
+    RowsArgs a{};
+    a.t[0] = RowsTensor{k.ptr, k_pages.ptr, k.stride_head, k.stride_token, k_pages.stride_head, k_pages.stride_slot, k_pages.stride_page, k_weight, k_bias,
+                        c.kv_heads, 0, rotary ? rot.norm : (int32_t)HTTM_NORM_NONE, rotary && rot.table.rotated_dim > 0};
+    a.t[1] = RowsTensor{v.ptr, v_pages.ptr, v.stride_head, v.stride_token, v_pages.stride_head, v_pages.stride_slot, v_pages.stride_page, nullptr, nullptr,
+                        c.kv_heads, 0, HTTM_NORM_NONE, 0};
+    if (rotary) {
+        a.table = rot.table;
+        a.eps = rot.eps;
+    }
+    a.positions = positions ? positions : part_of<int32_t>(b, b->at.positions);
+    a.slots = part_of<int32_t>(b, b->at.slots);
+    a.n_tokens = p.n_tokens;
+    a.page_shift = p.page_shift;
+    a.status = b->status;
+    return cuda_result(launch_rows(a, c.head_dim, dtype, b->sm_count, static_cast<cudaStream_t>(cuda_stream)), "append launch");
+}
+
+int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_pages v_pages, httm_tensor q, httm_tensor out, double scale,
+                         void* cuda_stream) {
+    if (int rc = check_common(b, dtype, "cache_attention")) return rc;
+    const httm_batch_config& c = b->cfg;
+    const BatchPlan& p = b->plan;
+    if (!std::isfinite(scale)) return global_fail(HTTM_ERR_INVALID_ARG, "cache_attention: scale must be finite");
+    int rc = check_pages(k_pages, c, "cache_attention: k_pages");
+    if (!rc) rc = check_pages(v_pages, c, "cache_attention: v_pages");
+    if (p.n_tokens == 0) return rc;
+    if (!rc) rc = check_rows_layout(q, c.heads, p.n_tokens, c.head_dim, false, "cache_attention: q");
+    if (!rc) rc = check_rows_layout(out, c.heads, p.n_tokens, c.head_dim, true, "cache_attention: out");
+    if (rc) return rc;
+    if (q.ptr == out.ptr || rows_conflict(q, c.heads, out, c.heads, p.n_tokens, c.head_dim))
+        return global_fail(HTTM_ERR_INVALID_ARG, "cache_attention: out overlaps q");
+    OnDevice guard(c.device);
+    if (!guard.ok) return global_fail(HTTM_ERR_CUDA, "cache_attention: cudaSetDevice failed");
+    CacheArgs a{};
+    a.segs = part_of<CacheSeg>(b, b->at.segs);
+    a.jobs = part_of<CacheJob>(b, b->at.narrow_jobs);
+    a.job_start = part_of<int32_t>(b, b->at.narrow_start);
+    a.table = part_of<int32_t>(b, b->at.table);
+    a.parts = part_of<int2>(b, b->at.parts);
+    a.prefix_seg = part_of<int32_t>(b, b->at.prefix_seg);
+    a.own_seg = part_of<int32_t>(b, b->at.own_seg);
+    a.q = q.ptr, a.k = k_pages.ptr, a.v = v_pages.ptr, a.out = out.ptr;
+    a.q_head = q.stride_head, a.q_token = q.stride_token, a.out_head = out.stride_head, a.out_token = out.stride_token;
+    a.k_page = k_pages.stride_page, a.k_head = k_pages.stride_head, a.k_slot = k_pages.stride_slot;
+    a.v_page = v_pages.stride_page, a.v_head = v_pages.stride_head, a.v_slot = v_pages.stride_slot;
+    a.partial = b->partial;
+    a.scale_log2 = (float)(scale * 1.4426950408889634);
+    a.group = c.heads / c.kv_heads;
+    a.kv_heads = c.kv_heads;
+    a.page_shift = p.page_shift;
+    a.n_tokens = p.n_tokens;
+    a.status = b->status;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!p.narrow_jobs.empty()) rc = cuda_result(launch_cache_narrow(a, c.head_dim, dtype, (int)p.narrow_start.size() - 1, stream), "cache_attention launch");
+    if (!rc && p.combine) rc = cuda_result(launch_cache_combine(a, c.head_dim, dtype, stream), "cache_attention launch");
+    return rc;
+}
+
+}  // extern "C"

@@ -1,0 +1,302 @@
+// The plan of a batch over a paged cache (host code, see httm_batch.cu): checks, row tiles, jobs and where everything lies in one block of memory.
+#pragma once
+
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <cmath>
+#include <functional>
+#include <queue>
+#include <string>
+#include <utility>
+#include <vector>
+
+#include "httm_cache.h"
+
+namespace httm {
+
+struct BatchInput {
+    int32_t n_sequences;
+    const int32_t *lengths, *queries, *tables;
+    int64_t table_stride;
+    const int32_t* prefix_pages;
+    int32_t prefix_length;
+};
+struct BatchPlan {
+    int32_t n_tokens = 0, page_shift = 0, part_units = 0;
+    int64_t last_position = -1;       // largest place of a new token behind the prefix
+    bool can_append = true, same_place = false, combine = false;
+    std::vector<CacheSeg> segs;
+    std::vector<CacheJob> narrow_jobs, wide_jobs;
+    std::vector<int32_t> narrow_start, wide_start;   // [CTAs + 1]
+    std::vector<int32_t> table, prefix_seg, own_seg, slots, positions;
+    std::vector<int2> parts;   // [row tile][kv head]
+};
+
+inline int32_t pages_of(int32_t length, int32_t page) { return (int32_t)(((int64_t)length + page - 1) / page); }
+
+inline int check_batch(const httm_batch_config& c, const BatchInput& in, std::string* why) {
+    auto bad = [&](int code, const char* msg) {
+        *why = msg;
+        return code;
+    };
+    auto pages_exist = [&](const int32_t* t, int32_t n) {
+        for (int32_t i = 0; i < n; ++i)
+            if (t[i] < 0 || t[i] >= c.n_pages) return false;
+        return true;
+    };
+    if (in.n_sequences < 0 || in.prefix_length < 0 || in.table_stride < 0) return bad(HTTM_ERR_INVALID_ARG, "a size is negative");
+    if (in.n_sequences > 0 && (!in.lengths || !in.queries)) return bad(HTTM_ERR_INVALID_ARG, "null array");
+    const int32_t n_prefix = pages_of(in.prefix_length, c.page_size);
+    if (n_prefix > 0 && !in.prefix_pages) return bad(HTTM_ERR_INVALID_ARG, "null array");
+    if (n_prefix > 0 && !pages_exist(in.prefix_pages, n_prefix)) return bad(HTTM_ERR_INVALID_ARG, "a page of the prefix does not exist");
+    int64_t tokens = 0, pages = n_prefix;
+    for (int32_t i = 0; i < in.n_sequences; ++i) {
+        if (in.lengths[i] < 0 || in.queries[i] < 0) return bad(HTTM_ERR_INVALID_ARG, "a length is negative");
+        const int32_t n = pages_of(in.lengths[i], c.page_size);
+        if (n > 0 && !in.tables) return bad(HTTM_ERR_INVALID_ARG, "null array");
+        if (n > in.table_stride) return bad(HTTM_ERR_INVALID_ARG, "a sequence has more pages than its row of the table");
+        if (!pages_exist(in.tables + i * in.table_stride, n)) return bad(HTTM_ERR_INVALID_ARG, "a page of a sequence does not exist");
+        if ((int64_t)in.lengths[i] + in.prefix_length > (1ll << 31) - 1 - kWideKeys) return bad(HTTM_ERR_UNSUPPORTED, "more than 2^31 keys");
+        tokens += in.queries[i];
+        pages += n;
+    }
+    if (tokens * c.heads > (1ll << 31) - 1) return bad(HTTM_ERR_UNSUPPORTED, "tokens * heads must be below 2^31");
+    if (pages > (1ll << 31) - 1) return bad(HTTM_ERR_UNSUPPORTED, "too many pages");
+    return HTTM_OK;
+}
+
+// Rows of a tile of the narrow kernel that holds `rows` rows of `group` heads; 0 if none does.
+inline int narrow_tile(int64_t tokens, int group) {
+    for (int r : {16, 32, 64})
+        if (tokens <= r / group) return r;
+    return 0;
+}
+
+// What is to be dealt: a row tile (or a pair of them) and a key head, `tiles` key tiles.
+struct BatchItem {
+    int32_t seg, head, pair, tiles;
+};
+
+// Deals items to `ctas` CTAs, see the top of httm_batch.cu.  `job_cost`: what starting and ending a job costs, in key tiles.
+struct Dealer {
+    std::vector<std::vector<CacheJob>> of;   // jobs of every CTA
+    BatchPlan* p;
+    int kv_heads;
+    void take(int cta, const BatchItem& it, int t0, int t1, bool whole) {
+        CacheJob j{};
+        j.seg = it.seg, j.head = it.head, j.pair = it.pair, j.tile0 = t0, j.tile1 = t1;
+        j.part = j.part2 = -1;
+        for (int k = 0; k <= it.pair; ++k) {
+            int2& parts = p->parts[(size_t)(it.seg + k) * kv_heads + it.head];
+            if (whole) {
+                parts.y = -1;
+            } else {
+                (k ? j.part2 : j.part) = parts.x + parts.y * (p->segs[it.seg + k].tile_rows / kPartUnit);
+                ++parts.y;
+            }
+        }
+        of[cta].push_back(j);
+    }
+    // sole[seg]: no other row tile holds its tokens
+    void deal(const std::vector<BatchItem>& items, const std::vector<char>& sole, int ctas, int job_cost, int least) {
+        of.assign(ctas, {});
+        if (items.empty()) return;
+        double total = 0;
+        for (const BatchItem& it : items) total += it.tiles + job_cost;
+        double quota = std::max(total / ctas, (double)(least + job_cost));
+        std::vector<double> load(ctas, 0.0);
+        std::priority_queue<std::pair<double, int>, std::vector<std::pair<double, int>>, std::greater<std::pair<double, int>>> idle;
+        for (int c = 0; c < ctas; ++c) idle.push({0.0, c});
+        std::vector<BatchItem> left;
+        std::vector<std::pair<BatchItem, int>> whole;
+        for (const BatchItem& it : items) {
+            const auto top = idle.top();
+            if (top.first + it.tiles + job_cost <= quota + 0.5 * least) {
+                idle.pop();
+                whole.push_back({it, top.second});
+                load[top.second] += it.tiles + job_cost;
+                idle.push({load[top.second], top.second});
+            } else {
+                left.push_back(it);
+            }
+        }
+        struct Piece {
+            BatchItem it;
+            int cta, t0, t1;
+        };
+        std::vector<Piece> pieces;
+        size_t next = 0;
+        int done = 0;   // key tiles of left[next] that are dealt
+        while (next < left.size()) {
+            for (int c = 0; c < ctas && next < left.size(); ++c) {
+                while (next < left.size()) {
+                    const int rest = left[next].tiles - done;
+                    const double room = quota - load[c] - job_cost;
+                    int n = room <= 0 ? 0 : (int)std::min((double)rest, std::ceil(room));
+                    if (n < rest && rest - n < least) n = rest - n <= least / 2 ? rest : n;   // no crumbs
+                    if (n < std::min(least, rest)) break;
+                    pieces.push_back({left[next], c, done, done + n});
+                    load[c] += n + job_cost;
+                    done += n;
+                    if (done == left[next].tiles) ++next, done = 0;
+                }
+            }
+            quota += std::max(1.0, 0.02 * quota);
+        }
+        // parts of one row tile and head lie side by side: count them first
+        std::vector<int> count((size_t)p->segs.size() * kv_heads, 0);
+        for (const auto& w : whole)
+            if (!sole[w.first.seg]) ++count[(size_t)w.first.seg * kv_heads + w.first.head];
+        for (const Piece& q : pieces) ++count[(size_t)q.it.seg * kv_heads + q.it.head];
+        auto place = [&](const BatchItem& it) {
+            for (int k = 0; k <= it.pair; ++k) {
+                int2& parts = p->parts[(size_t)(it.seg + k) * kv_heads + it.head];
+                if (parts.x >= 0) continue;
+                parts.x = p->part_units;
+                p->part_units += count[(size_t)it.seg * kv_heads + it.head] * (p->segs[it.seg + k].tile_rows / kPartUnit);
+            }
+        };
+        for (const auto& w : whole) {
+            const bool direct = sole[w.first.seg];
+            if (!direct) place(w.first), p->combine = true;
+            take(w.second, w.first, 0, w.first.tiles, direct);
+        }
+        for (const Piece& q : pieces) {
+            const bool direct = sole[q.it.seg] && q.t0 == 0 && q.t1 == q.it.tiles;
+            if (!direct) place(q.it), p->combine = true;
+            take(q.cta, q.it, q.t0, q.t1, direct);
+        }
+    }
+    void collect(std::vector<CacheJob>* jobs, std::vector<int32_t>* start) const {
+        jobs->clear();
+        start->assign(1, 0);
+        for (const auto& list : of) {
+            if (list.empty()) continue;
+            jobs->insert(jobs->end(), list.begin(), list.end());
+            start->push_back((int32_t)jobs->size());
+        }
+    }
+};
+
+inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, int sm_count, BatchPlan* p) {
+    const int group = c.heads / c.kv_heads, page = c.page_size, n_seq = in.n_sequences;
+    const int32_t prefix = in.prefix_length, n_prefix = pages_of(prefix, page);
+    *p = BatchPlan();
+    while ((1 << p->page_shift) < page) ++p->page_shift;
+    p->table.assign(in.prefix_pages, in.prefix_pages + n_prefix);
+    std::vector<int32_t> table_at(n_seq), token_at(n_seq), written;
+    for (int i = 0; i < n_seq; ++i) {
+        const int32_t length = in.lengths[i], nq = in.queries[i], n = pages_of(length, page);
+        const int32_t* t = in.tables + i * in.table_stride;
+        table_at[i] = (int32_t)p->table.size();
+        token_at[i] = p->n_tokens;
+        if (n > 0) p->table.insert(p->table.end(), t, t + n);
+        p->n_tokens += nq;
+        if (nq > length) {
+            p->can_append = false;
+            p->slots.resize(p->n_tokens, -1);
+            p->positions.resize(p->n_tokens, -1);
+            continue;
+        }
+        for (int32_t j = length - nq; j < length; ++j) {
+            p->slots.push_back(t[j / page] * page + j % page);
+            p->positions.push_back(prefix + j);
+        }
+        if (nq > 0) {
+            p->last_position = std::max<int64_t>(p->last_position, (int64_t)prefix + length - 1);
+            for (int32_t j = (length - nq) / page; j < n; ++j) written.push_back(t[j]);
+        }
+    }
+    if (!written.empty()) {
+        std::sort(written.begin(), written.end());
+        p->same_place = std::adjacent_find(written.begin(), written.end()) != written.end();
+        for (int32_t i = 0; i < n_prefix && !p->same_place; ++i) p->same_place = std::binary_search(written.begin(), written.end(), in.prefix_pages[i]);
+    }
+    // row tiles
+    p->prefix_seg.assign(p->n_tokens, -1);
+    p->own_seg.assign(p->n_tokens, -1);
+    std::vector<BatchItem> narrow;
+    std::vector<char> sole;
+    auto key_tiles = [&](const CacheSeg& s, int keys) { return (s.prefix_keys + keys - 1) / keys + (s.own_keys + keys - 1) / keys; };
+    auto add = [&](int32_t token0, int32_t tokens, int rows, int32_t prefix_keys, int seq, int32_t first_query) {
+        CacheSeg s{};
+        s.token0 = token0, s.tokens = tokens, s.tile_rows = rows, s.prefix_keys = prefix_keys;
+        if (seq >= 0) {
+            const int32_t length = in.lengths[seq];
+            s.own_table = table_at[seq];
+            s.seen0 = c.causal ? length - in.queries[seq] + first_query + 1 : length;
+            s.seen_step = c.causal;
+            s.own_keys = std::max<int32_t>(0, std::min<int64_t>(length, (int64_t)s.seen0 + (int64_t)(tokens - 1) * s.seen_step));
+        }
+        if (s.prefix_keys == 0 && s.own_keys == 0) return;
+        const int at = (int)p->segs.size();
+        p->segs.push_back(s);
+        for (int32_t t = token0; t < token0 + tokens; ++t) (seq >= 0 ? p->own_seg : p->prefix_seg)[t] = at;
+    };
+    int32_t run0 = 0, run = 0;   // tokens of consecutive sequences that leave the prefix to common row tiles
+    auto close_run = [&] {
+        if (run > 0 && prefix > 0) {
+            const int one = narrow_tile(run, group), rows = one ? one : 64, per = std::max(1, rows / group);
+            for (int32_t t = 0; t < run; t += per) add(run0 + t, std::min<int32_t>(per, run - t), rows, prefix, -1, 0);
+        }
+        run = 0;
+    };
+    for (int i = 0; i < n_seq; ++i) {
+        const int32_t nq = in.queries[i];
+        if (nq == 0) continue;
+        const int rows = narrow_tile(nq, group);
+        if (rows) {
+            if (run == 0) run0 = token_at[i];
+            run += nq;
+            add(token_at[i], nq, rows, 0, i, 0);
+        } else {
+            close_run();
+            const int per = std::max(1, 64 / group);
+            for (int32_t t = 0; t < nq; t += per) add(token_at[i] + t, std::min<int32_t>(per, nq - t), 64, prefix, i, t);
+        }
+    }
+    close_run();
+    sole.assign(p->segs.size(), 1);
+    for (int32_t t = 0; t < p->n_tokens; ++t) {
+        const int32_t a = p->prefix_seg[t], b = p->own_seg[t];
+        if (a >= 0 && b >= 0) sole[a] = sole[b] = 0;
+        if (a < 0 && b < 0) p->combine = true;   // (it writes the zeros of rows without keys)
+    }
+    p->parts.assign(p->segs.size() * c.kv_heads, int2{-1, 0});
+    for (int h = 0; h < c.kv_heads; ++h)
+        for (int s = 0; s < (int)p->segs.size(); ++s) narrow.push_back({s, h, 0, key_tiles(p->segs[s], kNarrowKeys)});
+    Dealer d;
+    d.p = p;
+    d.kv_heads = c.kv_heads;
+    d.deal(narrow, sole, 2 * sm_count, 2, 4);
+    d.collect(&p->narrow_jobs, &p->narrow_start);
+}
+
+// Where the parts of a plan lie in one block (offsets in bytes, multiples of 256).
+struct BatchLayout {
+    size_t segs = 0, narrow_jobs = 0, wide_jobs = 0, narrow_start = 0, wide_start = 0, table = 0, parts = 0, prefix_seg = 0, own_seg = 0, slots = 0, positions = 0,
+           bytes = 0;
+    BatchLayout() = default;
+    explicit BatchLayout(const BatchPlan& p) {
+        auto room = [&](size_t n) {
+            const size_t at = bytes;
+            bytes += (n + 255) & ~(size_t)255;
+            return at;
+        };
+        auto of = [&](const auto& v) { return room(v.size() * sizeof(v[0])); };
+        segs = of(p.segs), narrow_jobs = of(p.narrow_jobs), wide_jobs = of(p.wide_jobs), narrow_start = of(p.narrow_start), wide_start = of(p.wide_start);
+        table = of(p.table), parts = of(p.parts), prefix_seg = of(p.prefix_seg), own_seg = of(p.own_seg), slots = of(p.slots), positions = of(p.positions);
+        bytes += 256;
+    }
+    void write(const BatchPlan& p, unsigned char* to) const {
+        auto put = [&](size_t at, const auto& v) {
+            if (!v.empty()) memcpy(to + at, v.data(), v.size() * sizeof(v[0]));
+        };
+        put(segs, p.segs), put(narrow_jobs, p.narrow_jobs), put(wide_jobs, p.wide_jobs), put(narrow_start, p.narrow_start), put(wide_start, p.wide_start);
+        put(table, p.table), put(parts, p.parts), put(prefix_seg, p.prefix_seg), put(own_seg, p.own_seg), put(slots, p.slots), put(positions, p.positions);
+    }
+};
+
+}  // namespace httm

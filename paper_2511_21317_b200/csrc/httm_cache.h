@@ -1,0 +1,136 @@
+// Internal declarations of the operators around a kept scene: norms and rotation of queries and keys, the paged cache of keys and
+// values, attention of a batch to a shared prefix and to its own keys.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <string>
+
+#include "../../include/httm.h"
+
+namespace httm {
+
+void set_global_error(const std::string& msg);   // the text of httm_last_error(NULL), per thread
+int global_fail(int code, const char* fmt, ...);  // sets it and returns `code`
+
+struct OnDevice {   // the calling thread's current device for as long as it lives
+    int prev = -1;
+    bool ok = true;
+    explicit OnDevice(int dev) {
+        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
+        if (prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
+    }
+    ~OnDevice() {
+        int cur = -1;
+        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
+    }
+};
+
+// ---------------------------------------------------------------- rows: norms, rotation, append
+struct RowsTensor {
+    const void* in;
+    void* out;
+    int64_t in_head, in_token;               // element strides
+    int64_t out_head, out_token, out_page;   // (paged output: out_token is the stride between slots of a page)
+    const float *weight, *bias;              // [head_dim] or null
+    int32_t heads, chunks;                   // chunks of kHeadsPerChunk heads
+    int32_t norm;                            // HTTM_NORM_*
+    int32_t rotate;
+};
+struct RotationTable {
+    const float2* cos_sin;   // [n_positions][half]
+    int32_t n_positions, axes, half, rotated_dim, interleaved;
+};
+struct RowsArgs {
+    RowsTensor t[2];
+    RotationTable table;
+    const int32_t* positions;   // [tokens][axes]
+    const int32_t* slots;       // paged output: page * page_size + place of every token
+    int64_t n_tokens;
+    float eps;
+    int32_t page_shift;
+    int32_t* status;
+};
+struct RowsGradTensor {
+    const void *x, *dy;
+    void* dx;
+    int64_t x_head, x_token, dy_head, dy_token, dx_head, dx_token;
+    const float* weight;
+    float *dweight, *dbias;   // [head_dim] or null
+    int32_t heads, chunks;
+};
+struct RowsGradArgs {
+    RowsGradTensor t[2];
+    RotationTable table;
+    const int32_t* positions;
+    int64_t n_tokens;
+    float eps;
+    int32_t norm;
+    float* partial;     // [tensor][CTA][2][head_dim]
+    int32_t* arrived;   // [tensor], zero between launches
+    int32_t* status;
+};
+cudaError_t launch_rows(const RowsArgs& a, int head_dim, int dtype, int sm_count, cudaStream_t stream);
+cudaError_t launch_rows_grad(const RowsGradArgs& a, int head_dim, int dtype, int sm_count, cudaStream_t stream);
+size_t rows_grad_partial_floats(int head_dim, int sm_count);
+
+// What httm_cache_append needs of a rotary handle.
+struct RotaryView {
+    RotationTable table;
+    int32_t device, head_dim, norm;
+    float eps;
+};
+bool rotary_view(const httm_rotary* r, RotaryView* out);
+
+// Layout rules of a caller's tensor [heads][tokens][dim] of 16-bit elements through two element strides.
+int check_rows_layout(const httm_tensor& t, int64_t heads, int64_t tokens, int dim, bool written, const char* name);
+// Whether writing `y` could change what is still to be read through `x`: their extents overlap and they are not the same view.
+bool rows_conflict(const httm_tensor& x, int64_t x_heads, const httm_tensor& y, int64_t y_heads, int64_t tokens, int dim);
+
+// ---------------------------------------------------------------- attention over a paged cache: the plan and its kernels
+constexpr int kNarrowKeys = 64;    // keys of a tile of the narrow kernel
+constexpr int kWideKeys = 128;     // of the wide kernel
+constexpr int kWideRows = 128;     // query rows of a tile of the wide kernel; the narrow kernel has 16, 32 or 64
+constexpr int kPartUnit = 16;      // partial results are laid out in units of 16 rows of head_dim + 2 floats
+
+// A row tile and the keys its rows see.  Rows are (token, query head of the group), the group's heads of a token side by side.
+struct alignas(16) CacheSeg {
+    int32_t token0, tokens;     // the tokens of the tile
+    int32_t tile_rows;          // 16, 32, 64: narrow; 128: wide
+    int32_t prefix_keys;        // keys of the prefix (0: this tile does not look at it)
+    int32_t own_keys;           // most own keys that any of its tokens sees (0: none)
+    int32_t own_table;          // where the sequence's pages begin in the table
+    int32_t seen0, seen_step;   // token i of the tile sees min(own_keys, seen0 + i * seen_step) own keys
+};
+struct alignas(16) CacheJob {   // key tiles [tile0, tile1) of a row tile: those of the prefix, then the own ones
+    int32_t seg, head;
+    int32_t pair;               // wide: 1 if the job takes the row tile behind `seg` too
+    int32_t tile0, tile1;
+    int32_t part;               // first unit of its partial result; -1: it is the whole result and goes to `out`
+    int32_t part2;              // of the second row tile
+    int32_t pad;
+};
+struct CacheArgs {
+    const CacheSeg* segs;
+    const CacheJob* jobs;
+    const int32_t* job_start;   // [CTAs + 1]
+    const int32_t* table;       // pages of the prefix, then of every sequence
+    const int2* parts;          // [row tile][kv head]: first unit, number of partial results (-1: written by its job)
+    const int32_t *prefix_seg, *own_seg;   // [token]: the row tiles that hold it, or -1
+    const void *q, *k, *v;
+    void* out;
+    int64_t q_head, q_token, out_head, out_token;
+    int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
+    float* partial;
+    float scale_log2;
+    int32_t group, kv_heads, page_shift, n_tokens;
+    int32_t* status;
+};
+cudaError_t configure_cache_attention();
+cudaError_t launch_cache_narrow(const CacheArgs& a, int head_dim, int dtype, int ctas, cudaStream_t stream);
+cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, cudaStream_t stream);
+
+}  // namespace httm

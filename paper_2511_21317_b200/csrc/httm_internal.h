@@ -21,7 +21,8 @@ enum : int {
     kDevTimeoutAttention = 2,   // attention kernel: a pipeline barrier did not complete in time
     kDevBadIndex = 3,           // an index read from a map was out of range (skipped)
     kDevTimeoutBigMatch = 4,    // large-block score kernel: a pipeline barrier did not complete in time
-    kDevTimeoutLinear = 5       // projection GEMM: a pipeline barrier did not complete in time
+    kDevTimeoutLinear = 5,      // projection GEMM: a pipeline barrier did not complete in time
+    kDevTimeoutCache = 6        // attention over a paged cache: a pipeline barrier did not complete in time
 };
 
 // One merging block (Sec. 3.3): tokens [start, start + n) of the reordered sequence.
