@@ -420,7 +420,7 @@ typedef struct httm_batch httm_batch; /* opaque: the sequences of one step, thei
 
 typedef struct {
     int32_t device;
-    int32_t heads, kv_heads; /* heads a multiple of kv_heads, at most 64 query heads to a key head                 */
+    int32_t heads, kv_heads; /* heads a multiple of kv_heads, at most 128 query heads to a key head                 */
     int32_t head_dim;        /* 64 or 128                                                                         */
     int32_t page_size;       /* tokens of a page: 16, 32, 64, 128 or 256                                          */
     int32_t causal;          /* 1: of its own keys a query sees those up to its own place; 0: all of them         */

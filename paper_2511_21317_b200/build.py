@@ -19,7 +19,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libhttm.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["httm_api.cu", "httm_small_blocks.cu", "httm_mid_blocks.cu", "httm_mem_kernels.cu", "httm_attention_tc.cu", "httm_big_blocks.cu", "httm_linear.cu", "httm_static.cu",
-           "httm_umma_selftest.cu", "httm_rotary.cu", "httm_batch.cu", "httm_cache_narrow.cu"]
+           "httm_umma_selftest.cu", "httm_rotary.cu", "httm_batch.cu", "httm_cache_narrow.cu", "httm_cache_wide.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",

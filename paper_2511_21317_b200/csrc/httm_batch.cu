@@ -108,7 +108,7 @@ int httm_batch_create(const httm_batch_config* config, httm_batch** out) {
     const httm_batch_config& c = *config;
     if (c.heads < 1 || c.kv_heads < 1 || c.heads % c.kv_heads != 0 || c.heads > 65535)
         return global_fail(HTTM_ERR_INVALID_ARG, "batch: heads must be a positive multiple of kv_heads");
-    if (c.heads / c.kv_heads > 64) return global_fail(HTTM_ERR_UNSUPPORTED, "batch: at most 64 query heads to a key head");
+    if (c.heads / c.kv_heads > kWideRows) return global_fail(HTTM_ERR_UNSUPPORTED, "batch: at most 128 query heads to a key head");
     if (c.head_dim != 64 && c.head_dim != 128) return global_fail(HTTM_ERR_UNSUPPORTED, "batch: head_dim must be 64 or 128");
     if (c.page_size != 16 && c.page_size != 32 && c.page_size != 64 && c.page_size != 128 && c.page_size != 256)
         return global_fail(HTTM_ERR_UNSUPPORTED, "batch: page_size must be 16, 32, 64, 128 or 256");
@@ -127,6 +127,7 @@ int httm_batch_create(const httm_batch_config* config, httm_batch** out) {
     if (!rc) rc = cuda_result(cudaMemset(b->status, 0, sizeof(int32_t)), "batch");
     if (!rc) rc = cuda_result(cudaEventCreateWithFlags(&b->uploaded, cudaEventDisableTiming), "batch");
     if (!rc) rc = cuda_result(configure_cache_attention(), "batch");
+    if (!rc) rc = cuda_result(configure_cache_wide(), "batch");
     if (!rc) rc = cuda_result(cudaDeviceSynchronize(), "batch");
     if (rc) {
         delete b;
@@ -238,7 +239,7 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
     int rc = check_pages(k_pages, c, "cache_attention: k_pages");
     if (!rc) rc = check_pages(v_pages, c, "cache_attention: v_pages");
     if (p.n_tokens == 0) return rc;
-    if (!rc) rc = check_rows_layout(q, c.heads, p.n_tokens, c.head_dim, false, "cache_attention: q");
+    if (!rc) rc = check_rows_layout(q, c.heads, p.n_tokens, c.head_dim, true, "cache_attention: q");   // (tensor maps have no broadcast dimensions)
     if (!rc) rc = check_rows_layout(out, c.heads, p.n_tokens, c.head_dim, true, "cache_attention: out");
     if (rc) return rc;
     if (q.ptr == out.ptr || rows_conflict(q, c.heads, out, c.heads, p.n_tokens, c.head_dim))
@@ -265,7 +266,13 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
     a.n_tokens = p.n_tokens;
     a.status = b->status;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (!p.narrow_jobs.empty()) rc = cuda_result(launch_cache_narrow(a, c.head_dim, dtype, (int)p.narrow_start.size() - 1, stream), "cache_attention launch");
+    if (!p.wide_jobs.empty()) {
+        CacheArgs w = a;
+        w.jobs = part_of<CacheJob>(b, b->at.wide_jobs);
+        w.job_start = part_of<int32_t>(b, b->at.wide_start);
+        rc = cuda_result(launch_cache_wide(w, c.head_dim, dtype, c.n_pages, (int)p.wide_start.size() - 1, stream), "cache_attention launch");
+    }
+    if (!rc && !p.narrow_jobs.empty()) rc = cuda_result(launch_cache_narrow(a, c.head_dim, dtype, (int)p.narrow_start.size() - 1, stream), "cache_attention launch");
     if (!rc && p.combine) rc = cuda_result(launch_cache_combine(a, c.head_dim, dtype, stream), "cache_attention launch");
     return rc;
 }

@@ -77,9 +77,11 @@ inline int narrow_tile(int64_t tokens, int group) {
 // What is to be dealt: a row tile (or a pair of them) and a key head, `tiles` key tiles.
 struct BatchItem {
     int32_t seg, head, pair, tiles;
+    double cost;   // of a key tile
 };
 
-// Deals items to `ctas` CTAs, see the top of httm_batch.cu.  `job_cost`: what starting and ending a job costs, in key tiles.
+// Deals items to `ctas` CTAs, see the top of httm_batch.cu.  `job_cost`: what starting and ending a job costs; `least`: key tiles of the shortest job that
+// is cut off.
 struct Dealer {
     std::vector<std::vector<CacheJob>> of;   // jobs of every CTA
     BatchPlan* p;
@@ -104,8 +106,8 @@ struct Dealer {
         of.assign(ctas, {});
         if (items.empty()) return;
         double total = 0;
-        for (const BatchItem& it : items) total += it.tiles + job_cost;
-        double quota = std::max(total / ctas, (double)(least + job_cost));
+        for (const BatchItem& it : items) total += it.tiles * it.cost + job_cost;
+        double quota = std::max(total / ctas, least * items[0].cost + job_cost);
         std::vector<double> load(ctas, 0.0);
         std::priority_queue<std::pair<double, int>, std::vector<std::pair<double, int>>, std::greater<std::pair<double, int>>> idle;
         for (int c = 0; c < ctas; ++c) idle.push({0.0, c});
@@ -113,10 +115,10 @@ struct Dealer {
         std::vector<std::pair<BatchItem, int>> whole;
         for (const BatchItem& it : items) {
             const auto top = idle.top();
-            if (top.first + it.tiles + job_cost <= quota + 0.5 * least) {
+            if (top.first + it.tiles * it.cost + job_cost <= quota + 0.5 * least * it.cost) {
                 idle.pop();
                 whole.push_back({it, top.second});
-                load[top.second] += it.tiles + job_cost;
+                load[top.second] += it.tiles * it.cost + job_cost;
                 idle.push({load[top.second], top.second});
             } else {
                 left.push_back(it);
@@ -134,11 +136,11 @@ struct Dealer {
                 while (next < left.size()) {
                     const int rest = left[next].tiles - done;
                     const double room = quota - load[c] - job_cost;
-                    int n = room <= 0 ? 0 : (int)std::min((double)rest, std::ceil(room));
+                    int n = room <= 0 ? 0 : (int)std::min((double)rest, std::ceil(room / left[next].cost));
                     if (n < rest && rest - n < least) n = rest - n <= least / 2 ? rest : n;   // no crumbs
                     if (n < std::min(least, rest)) break;
                     pieces.push_back({left[next], c, done, done + n});
-                    load[c] += n + job_cost;
+                    load[c] += n * left[next].cost + job_cost;
                     done += n;
                     if (done == left[next].tiles) ++next, done = 0;
                 }
@@ -217,7 +219,8 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     // row tiles
     p->prefix_seg.assign(p->n_tokens, -1);
     p->own_seg.assign(p->n_tokens, -1);
-    std::vector<BatchItem> narrow;
+    std::vector<BatchItem> narrow, wide;
+    std::vector<std::pair<int, int>> pairs;   // wide: (row tile, 1 if the next one goes with it)
     std::vector<char> sole;
     auto key_tiles = [&](const CacheSeg& s, int keys) { return (s.prefix_keys + keys - 1) / keys + (s.own_keys + keys - 1) / keys; };
     auto add = [&](int32_t token0, int32_t tokens, int rows, int32_t prefix_keys, int seq, int32_t first_query) {
@@ -238,7 +241,7 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     int32_t run0 = 0, run = 0;   // tokens of consecutive sequences that leave the prefix to common row tiles
     auto close_run = [&] {
         if (run > 0 && prefix > 0) {
-            const int one = narrow_tile(run, group), rows = one ? one : 64, per = std::max(1, rows / group);
+            const int one = narrow_tile(run, group), rows = one ? one : kWideRows, per = rows / group;
             for (int32_t t = 0; t < run; t += per) add(run0 + t, std::min<int32_t>(per, run - t), rows, prefix, -1, 0);
         }
         run = 0;
@@ -253,8 +256,8 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
             add(token_at[i], nq, rows, 0, i, 0);
         } else {
             close_run();
-            const int per = std::max(1, 64 / group);
-            for (int32_t t = 0; t < nq; t += per) add(token_at[i] + t, std::min<int32_t>(per, nq - t), 64, prefix, i, t);
+            const int per = kWideRows / group;
+            for (int32_t t = 0; t < nq; t += per) add(token_at[i] + t, std::min<int32_t>(per, nq - t), kWideRows, prefix, i, t);
         }
     }
     close_run();
@@ -265,11 +268,27 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
         if (a < 0 && b < 0) p->combine = true;   // (it writes the zeros of rows without keys)
     }
     p->parts.assign(p->segs.size() * c.kv_heads, int2{-1, 0});
-    for (int h = 0; h < c.kv_heads; ++h)
-        for (int s = 0; s < (int)p->segs.size(); ++s) narrow.push_back({s, h, 0, key_tiles(p->segs[s], kNarrowKeys)});
+    // Two row tiles of 128 rows form a pair if they look at the same keys (a pair walks those of the second one, which sees at least as many) and are dealt
+    // alike; a pair's key tile takes twice as long as a single's.
+    for (int s = 0; s < (int)p->segs.size(); ++s) {
+        const CacheSeg& a = p->segs[s];
+        if (a.tile_rows != kWideRows) continue;
+        const bool pair = s + 1 < (int)p->segs.size() && p->segs[s + 1].tile_rows == kWideRows && p->segs[s + 1].prefix_keys == a.prefix_keys &&
+                          (p->segs[s + 1].own_keys > 0) == (a.own_keys > 0) && p->segs[s + 1].own_table == a.own_table &&
+                          p->segs[s + 1].token0 == a.token0 + a.tokens && sole[s + 1] == sole[s];
+        pairs.push_back({s, pair ? 1 : 0});
+        if (pair) ++s;
+    }
+    for (int h = 0; h < c.kv_heads; ++h) {
+        for (int s = 0; s < (int)p->segs.size(); ++s)
+            if (p->segs[s].tile_rows != kWideRows) narrow.push_back({s, h, 0, key_tiles(p->segs[s], kNarrowKeys), 1.0});
+        for (const auto& w : pairs) wide.push_back({w.first, h, w.second, key_tiles(p->segs[w.first + w.second], kWideKeys), w.second ? 2.0 : 1.0});
+    }
     Dealer d;
     d.p = p;
     d.kv_heads = c.kv_heads;
+    d.deal(wide, sole, sm_count, 6, 4);
+    d.collect(&p->wide_jobs, &p->wide_start);
     d.deal(narrow, sole, 2 * sm_count, 2, 4);
     d.collect(&p->narrow_jobs, &p->narrow_start);
 }

@@ -131,6 +131,8 @@ struct CacheArgs {
 };
 cudaError_t configure_cache_attention();
 cudaError_t launch_cache_narrow(const CacheArgs& a, int head_dim, int dtype, int ctas, cudaStream_t stream);
+cudaError_t configure_cache_wide();
+cudaError_t launch_cache_wide(const CacheArgs& a, int head_dim, int dtype, int64_t n_pages, int ctas, cudaStream_t stream);
 cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, cudaStream_t stream);
 
 }  // namespace httm

@@ -1,0 +1,566 @@
+// Attention over a paged cache for row tiles of 128 rows (images, prompts, many sequences behind one prefix) on the 5th-generation tensor cores.
+//
+// One CTA per SM walks its jobs.  A job is a PAIR of row tiles (A, B) that share a stream of keys, or a SINGLE row tile whose even key tiles go to
+// softmax group A and whose odd ones go to group B (two softmaxes over disjoint keys, combined at the end).  Either way score tile k belongs to
+// group k mod 2 and lies in score buffer k mod NB of tensor memory:
+//   warp 0      producer: Q tiles once, then a ring of K and V tiles of 128 keys, page by page (TMA, 128-byte swizzle)
+//   warp 1      issues the products S = Q K^T (operands in shared memory) and O += P V (P in tensor memory over its S, V from shared memory)
+//   warps 2-5   softmax of group A, one thread per row: S from tensor memory, weights back as pairs of 16 bits; warps 6-9 of group B
+// S(k + NB) is issued right behind P(k) V into the buffer that this frees.  Tensor memory: NB score buffers of 128 columns and two accumulators of D, 512
+// columns in all (NB = 3 for 64 channels, 2 for 128; the ring has as many stages, 128 and 192 KB with the Q tiles).
+//
+// Q comes in boxes of (channels, heads of the group, tokens), so the rows of a tile are (token, head) whatever the group's size and the tensor's
+// strides; rows that a tile does not fill compute something that nobody stores.  Keys behind the end of the prefix or of a sequence are masked
+// by -inf, and the values in their places are set to zero in shared memory, because pages hold anything there and 0 x NaN is not 0.
+//
+// A row's stabiliser is the largest score at the time it was set, and is raised only when a tile exceeds it by more than 2^8: weights of up to
+// 2^8 cost no precision (they are rounded relative to themselves, and sums are 32-bit), and raising it rewrites the accumulator.
+#include <type_traits>
+
+#include "httm_cache.h"
+#include "httm_internal.h"
+#include "httm_launch.cuh"
+#include "tc_exp2.cuh"
+#include "tc_sm100.cuh"
+
+namespace httm {
+
+namespace {
+
+constexpr int BM = kWideRows, BN = kWideKeys;
+constexpr int kThreads = 320;
+constexpr int kTmemColumns = 512;
+constexpr int kSubTile = BM * 128;   // 128 rows of 64 channels
+constexpr int kPColumn = 64;         // P (16-bit pairs, 64 columns) lies over the last 64 columns of its S
+constexpr float kRaise = 8.f;        // in units of log2
+
+template <int D>
+struct Shape {
+    static constexpr int NB = D == 64 ? 3 : 2;   // score buffers, and stages of the ring
+    static constexpr int SUB = D / 64;           // 64-channel parts of a tile
+    static constexpr int TILE = SUB * kSubTile;
+    static constexpr int SMEM = (2 + 2 * NB) * TILE + 1024 /*alignment*/ + 512 /*barriers*/ + BM * 8 /*exchange*/;
+};
+
+template <int NB>
+struct Barriers {
+    uint64_t q_full, q_free;
+    uint64_t k_full[NB], k_empty[NB], v_full[NB], v_empty[NB];
+    uint64_t v_tail;                 // a V tile that needs zeros has arrived
+    uint64_t s_full[NB], p_full[NB];
+    uint64_t o_done[2];              // one completion per P V of the group
+    uint64_t o_final;
+    uint64_t x_full, x_done;         // single: group B's (maximum, sum) published / group A done with O_B
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {   // not a number if one of them is not
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+        : "memory");
+}
+template <int NB>
+__device__ __forceinline__ uint32_t uses(int n, int r) {   // how many of 0 .. n - 1 are r modulo NB
+    return (uint32_t)((n - r + NB - 1) / NB);
+}
+
+struct KeyTile {
+    int key0, keys;     // first key in the prefix / in the sequence; keys of the tile
+    int table;          // where its pages begin in the table
+    bool own;
+};
+__device__ __forceinline__ KeyTile key_tile(const CacheSeg& seg, int tile) {
+    const int n_prefix = (seg.prefix_keys + BN - 1) / BN;
+    KeyTile t;
+    t.own = tile >= n_prefix;
+    t.key0 = (t.own ? tile - n_prefix : tile) * BN;
+    t.keys = min(BN, (t.own ? seg.own_keys : seg.prefix_keys) - t.key0);
+    t.table = t.own ? seg.own_table : 0;
+    return t;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 1)
+cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                  const __grid_constant__ CacheArgs a) {
+    using S = Shape<D>;
+    constexpr int NB = S::NB, SUB = S::SUB, TILE = S::TILE;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const uint32_t s_q = tc::smem_addr(smem), s_k = s_q + 2 * TILE, s_v = s_k + NB * TILE;
+    Barriers<NB>* bars = reinterpret_cast<Barriers<NB>*>(smem + (2 + 2 * NB) * TILE);
+    static_assert(sizeof(Barriers<NB>) <= 512, "the barriers have 512 bytes");
+    volatile int* abort_flag = &bars->abort_flag;
+    auto bar = [](const uint64_t& b) { return tc::smem_addr(&b); };
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        bars->abort_flag = 0;
+        tc::mbar_init(bar(bars->q_full), 1);
+        tc::mbar_init(bar(bars->q_free), 1);
+        for (int i = 0; i < NB; ++i) {
+            tc::mbar_init(bar(bars->k_full[i]), 1);
+            tc::mbar_init(bar(bars->k_empty[i]), 1);
+            tc::mbar_init(bar(bars->v_full[i]), 1);
+            tc::mbar_init(bar(bars->v_empty[i]), 1);
+            tc::mbar_init(bar(bars->s_full[i]), 1);
+            tc::mbar_init(bar(bars->p_full[i]), BM);
+        }
+        tc::mbar_init(bar(bars->v_tail), 1);
+        tc::mbar_init(bar(bars->o_done[0]), 1);
+        tc::mbar_init(bar(bars->o_done[1]), 1);
+        tc::mbar_init(bar(bars->o_final), 1);
+        tc::mbar_init(bar(bars->x_full), BM);
+        tc::mbar_init(bar(bars->x_done), BM);
+        tc::fence_barrier_init();
+        tc::prefetch_tensormap(&map_q);
+        tc::prefetch_tensormap(&map_k);
+        tc::prefetch_tensormap(&map_v);
+    }
+    if (warp == 1) tc::tmem_alloc(tc::smem_addr(&bars->tmem_base), kTmemColumns);
+    depend_wait();
+    dependents_launch();
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tmem = bars->tmem_base;
+    const int job_first = ld_global(a.job_start + blockIdx.x), job_last = ld_global(a.job_start + blockIdx.x + 1);
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ producer (all lanes walk and wait, lane 0 issues)
+        const int page = 1 << a.page_shift, box = min(page, BN);
+        const uint32_t box_bytes = (uint32_t)box * 128u, q_bytes = (uint32_t)((BM / a.group) * a.group) * 128u * SUB;
+        uint32_t kv_base[NB] = {};       // key tiles of earlier jobs in every stage
+        uint32_t tails = 0;              // V tiles that got zeros
+        uint32_t k_loads[NB] = {}, v_loads[NB] = {}, q_loads = 0;   // completions that the loads issued so far bring to the barriers
+        bool ok = true;
+        for (int j = job_first; ok && j < job_last; ++j) {
+            const CacheJob job = a.jobs[j];
+            const CacheSeg seg = a.segs[job.seg + job.pair];   // (of a pair the second row tile sees the most keys)
+            const int token_a = job.pair ? a.segs[job.seg].token0 : seg.token0;
+            if (q_loads > 0 && !(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->q_free), (q_loads - 1) & 1u, abort_flag)))) break;
+            if (lane == 0) {
+                tc::mbar_expect_tx(bar(bars->q_full), job.pair ? 2 * q_bytes : q_bytes);
+                for (int x = 0; x <= job.pair; ++x)
+                    for (int c = 0; c < SUB; ++c)
+                        tma_load_4d(s_q + x * TILE + c * kSubTile, &map_q, bar(bars->q_full), 64 * c, 0, x ? seg.token0 : token_a, job.head);
+            }
+            ++q_loads;
+            const int n = job.tile1 - job.tile0;
+#pragma unroll 1
+            for (int i0 = 0; ok && i0 < n; i0 += NB) {
+#pragma unroll
+                for (int st = 0; st < NB; ++st) {   // key tile i of the job goes to stage i mod NB
+                    const int i = i0 + st;
+                    if (!ok || i >= n) break;
+                    const uint32_t fill = kv_base[st] + (uint32_t)(i0 / NB), par = (fill & 1u) ^ 1u;
+                    const KeyTile t = key_tile(seg, job.tile0 + i);
+                    const int boxes = (t.keys + box - 1) / box;
+                    const int32_t* pages = a.table + t.table + (t.key0 >> a.page_shift);
+                    const int slot = t.key0 & (page - 1);   // (pages of 256: the second half)
+                    auto load = [&](uint32_t dst, const CUtensorMap* map, uint32_t b) {
+                        for (int p = 0; p < boxes; ++p) {
+                            const int32_t id = ld_global(pages + p);
+                            for (int c = 0; c < SUB; ++c) tma_load_4d(dst + c * kSubTile + p * box_bytes, map, b, 64 * c, slot, job.head, id);
+                        }
+                    };
+                    if (fill > 0 && !(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->k_empty[st]), par, abort_flag)))) break;
+                    if (lane == 0) {
+                        tc::mbar_expect_tx(bar(bars->k_full[st]), boxes * SUB * box_bytes);
+                        load(s_k + st * TILE, &map_k, bar(bars->k_full[st]));
+                    }
+                    k_loads[st] = fill + 1;
+                    if (fill > 0 && !(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->v_empty[st]), par, abort_flag)))) break;
+                    const bool tail = t.keys < BN;
+                    if (lane == 0) {
+                        const uint32_t b = tail ? bar(bars->v_tail) : bar(bars->v_full[st]);
+                        tc::mbar_expect_tx(b, boxes * SUB * box_bytes);
+                        load(s_v + st * TILE, &map_v, b);
+                    }
+                    if (!tail) {
+                        v_loads[st] = fill + 1;
+                        continue;
+                    }
+                    __syncwarp();
+                    ++tails;
+                    if (!(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->v_tail), (tails - 1) & 1u, abort_flag)))) break;
+                    unsigned char* rows = smem + (2 + NB + st) * TILE;
+                    for (int c = 0; c < SUB; ++c)
+                        for (int at = t.keys * 8 + lane; at < BN * 8; at += 32) *reinterpret_cast<uint4*>(rows + c * kSubTile + at * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(bar(bars->v_full[st]));
+                }
+            }
+#pragma unroll
+            for (int st = 0; st < NB; ++st) kv_base[st] += uses<NB>(n, st);
+        }
+        if (!ok) {   // somebody gave up: what is still on its way has to land before the CTA leaves
+            if (lane == 0) {
+                auto landed = [&](uint64_t& b, uint32_t completions) {
+                    int gone = 0;   // (a flag of its own: with the common one set nobody waits any more)
+                    if (completions > 0) tc::mbar_wait(bar(b), (completions - 1) & 1u, &gone);
+                };
+                landed(bars->q_full, q_loads);
+                landed(bars->v_tail, tails);
+#pragma unroll
+                for (int st = 0; st < NB; ++st) {
+                    landed(bars->k_full[st], k_loads[st]);
+                    landed(bars->v_full[st], v_loads[st]);
+                }
+            }
+            __syncwarp();
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ products
+        if (tc::elect_one()) {
+            constexpr bool kHalf = std::is_same<T, __half>::value;
+            constexpr uint32_t kTypes = (1u << 7) | (1u << 10);   // A and B are bf16; without these bits fp16
+            constexpr uint32_t idesc_qk = tc::idesc_bf16(BM, BN, false, false) & ~(kHalf ? kTypes : 0u);
+            constexpr uint32_t idesc_pv = tc::idesc_bf16(BM, 64, false, true) & ~(kHalf ? kTypes : 0u);
+            const uint64_t dq0 = tc::smem_desc_sw128(s_q), dk0 = tc::smem_desc_sw128(s_k), dv0 = tc::smem_desc_sw128(s_v);
+            constexpr uint64_t kTileStep = TILE >> 4, kSubStep = kSubTile >> 4;   // descriptors count 16-byte units
+            auto issue_qk = [&](uint32_t t_s, uint64_t dq, uint64_t dk, uint32_t b) {
+#pragma unroll
+                for (int c = 0; c < SUB; ++c) {
+                    if (c == 0)
+                        tc::mma_ss_c<false>(t_s, dq, dk, idesc_qk);
+                    else
+                        tc::mma_ss_c<true>(t_s, dq + c * kSubStep, dk + c * kSubStep, idesc_qk);
+#pragma unroll
+                    for (int k = 1; k < 4; ++k) tc::mma_ss_c<true>(t_s, dq + c * kSubStep + 2 * k, dk + c * kSubStep + 2 * k, idesc_qk);
+                }
+                tc::mma_commit(b);
+            };
+            auto issue_pv = [&](uint32_t t_o, uint32_t t_p, uint64_t dv) {
+#pragma unroll
+                for (int c = 0; c < SUB; ++c)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) tc::mma_ts_c<true>(t_o + 64 * c, t_p + 8 * k, dv + c * kSubStep + (uint64_t)(k * 128), idesc_pv);
+            };
+            uint32_t kv_base[NB] = {}, sp_base[NB] = {};   // completions before this job: ring stages, score buffers
+            // score tile k = k0 + C of a pair, k0 a multiple of 2 NB (round: parity of k0 / (2 NB))
+            auto step_pair = [&](auto c_c, int k0, uint32_t round, int n_score) -> bool {
+                constexpr int C = decltype(c_c)::value;
+                constexpr int B = C % NB, X = C % 2, ST = (C >> 1) % NB;
+                constexpr int XN = (C + NB) % 2, JN = (C + NB) >> 1, STN = JN % NB;   // score tile k + NB: the next in this buffer
+                const uint32_t t_buf = tmem + B * BN, t_o = tmem + NB * BN + X * D;
+                if (X == 0 && !tc::mbar_wait(bar(bars->v_full[ST]), (kv_base[ST] + round) & 1u, abort_flag)) return false;
+                if (!tc::mbar_wait(bar(bars->p_full[B]), (sp_base[B] + (C / NB)) & 1u, abort_flag)) return false;
+                tc::fence_after_sync();
+                issue_pv(t_o, t_buf + kPColumn, dv0 + ST * kTileStep);
+                tc::mma_commit(bar(bars->o_done[X]));
+                if (X == 1) tc::mma_commit(bar(bars->v_empty[ST]));
+                if (k0 + C + NB < n_score) {
+                    if (XN == 0) {
+                        if (!tc::mbar_wait(bar(bars->k_full[STN]), (kv_base[STN] + round + (JN >= NB ? 1u : 0u)) & 1u, abort_flag)) return false;
+                        tc::fence_after_sync();
+                    }
+                    issue_qk(t_buf, dq0 + XN * kTileStep, dk0 + STN * kTileStep, bar(bars->s_full[B]));
+                    if (XN == 1) tc::mma_commit(bar(bars->k_empty[STN]));
+                    if (k0 + C + NB + 1 == n_score) tc::mma_commit(bar(bars->q_free));   // that was the job's last S
+                }
+                return true;
+            };
+            // score tile k = key tile k = k0 + C of a single row tile, k0 a multiple of 2 NB
+            auto step_single = [&](auto c_c, int k0, int n_single) -> bool {
+                constexpr int C = decltype(c_c)::value;
+                constexpr int B = C % NB, X = C % 2;
+                constexpr uint32_t IDX = C / NB;
+                const uint32_t t_buf = tmem + B * BN, t_o = tmem + NB * BN + X * D;
+                if (!tc::mbar_wait(bar(bars->v_full[B]), (kv_base[B] + IDX) & 1u, abort_flag)) return false;
+                if (!tc::mbar_wait(bar(bars->p_full[B]), (sp_base[B] + IDX) & 1u, abort_flag)) return false;
+                tc::fence_after_sync();
+                issue_pv(t_o, t_buf + kPColumn, dv0 + B * kTileStep);
+                tc::mma_commit(bar(bars->o_done[X]));
+                tc::mma_commit(bar(bars->v_empty[B]));
+                if (k0 + C + NB < n_single) {
+                    if (!tc::mbar_wait(bar(bars->k_full[B]), (kv_base[B] + IDX + 1u) & 1u, abort_flag)) return false;
+                    tc::fence_after_sync();
+                    issue_qk(t_buf, dq0, dk0 + B * kTileStep, bar(bars->s_full[B]));
+                    tc::mma_commit(bar(bars->k_empty[B]));
+                    if (k0 + C + NB + 1 == n_single) tc::mma_commit(bar(bars->q_free));
+                }
+                return true;
+            };
+            bool ok = true;
+            int jobs = 0;
+            for (int j = job_first; ok && j < job_last; ++j, ++jobs) {
+                const CacheJob job = a.jobs[j];
+                const int n = job.tile1 - job.tile0, n_score = job.pair ? 2 * n : n;
+                ok = tc::mbar_wait(bar(bars->q_full), (uint32_t)jobs & 1u, abort_flag);
+                if (!ok) break;
+                // prologue: S(0) .. S(NB - 1)
+#pragma unroll
+                for (int k = 0; k < NB; ++k) {
+                    if (k >= n_score) break;
+                    const int tile = job.pair ? k >> 1 : k, x = job.pair ? k & 1 : 0;
+                    if (x == 0) {
+                        if (!(ok = tc::mbar_wait(bar(bars->k_full[tile]), kv_base[tile] & 1u, abort_flag))) break;
+                        tc::fence_after_sync();
+                    }
+                    issue_qk(tmem + k * BN, dq0 + x * kTileStep, dk0 + tile * kTileStep, bar(bars->s_full[k]));
+                    if (!job.pair || x == 1) tc::mma_commit(bar(bars->k_empty[tile]));
+                    if (k + 1 == n_score) tc::mma_commit(bar(bars->q_free));
+                }
+                if (!ok) break;
+                uint32_t round = 0;
+                for (int k0 = 0; ok && k0 < n_score; k0 += 2 * NB, round ^= 1u) {
+                    auto run = [&](auto c_c) {
+                        if (ok && k0 + decltype(c_c)::value < n_score)
+                            ok = job.pair ? step_pair(c_c, k0, round, n_score) : step_single(c_c, k0, n_score);
+                    };
+                    run(std::integral_constant<int, 0>{});
+                    run(std::integral_constant<int, 1>{});
+                    run(std::integral_constant<int, 2>{});
+                    run(std::integral_constant<int, 3>{});
+                    if constexpr (NB == 3) {
+                        run(std::integral_constant<int, 4>{});
+                        run(std::integral_constant<int, 5>{});
+                    }
+                }
+                if (ok) tc::mma_commit(bar(bars->o_final));
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    sp_base[b] += uses<NB>(n_score, b);
+                    kv_base[b] += uses<NB>(n, b);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ softmax and results
+        const int x = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;   // group; row of the tile = lane of tensor memory
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t_o = tmem + NB * BN + x * D + lane_addr;
+        uint32_t sp_base[NB] = {}, od_base = 0, singles = 0;
+        float2* xch = reinterpret_cast<float2*>(smem + (2 + 2 * NB) * TILE + 512);
+        bool ok = true;
+        int jobs = 0;
+        for (int jb = job_first; ok && jb < job_last; ++jb, ++jobs) {
+            const CacheJob job = a.jobs[jb];
+            const CacheSeg keys_seg = a.segs[job.seg + job.pair], seg = a.segs[job.seg + (job.pair ? x : 0)];
+            const int n = job.tile1 - job.tile0, n_score = job.pair ? 2 * n : n, n_own = job.pair ? n : (n - x + 1) / 2;
+            const int token = row / a.group, head = job.head * a.group + row % a.group;
+            const bool exists = token < seg.tokens;
+            const int seen = exists ? min(seg.own_keys, seg.seen0 + token * seg.seen_step) : 0;
+            float m = -INFINITY, l = 0.f;
+            {   // the accumulator starts at zero: every P V adds to it (ordered before the first arrival at p_full)
+                uint32_t z[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) z[i] = 0u;
+#pragma unroll
+                for (int c = 0; c < D; c += 32) tc::tmem_st32(t_o + c, z);
+                if (n_own == 0) tc::tmem_wait_st();
+            }
+            for (int j = 0; j < n_own; ++j) {
+                const int k = 2 * j + x, buf = k % NB;
+                const uint32_t t_s = tmem + buf * BN + lane_addr;
+                const KeyTile t = key_tile(keys_seg, job.tile0 + (job.pair ? j : k));
+                const int limit = t.own ? min(t.keys, seen - t.key0) : (seg.prefix_keys > 0 ? t.keys : 0);
+                if (!(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->s_full[buf]), (sp_base[buf] + (uint32_t)(k / NB)) & 1u, abort_flag)))) break;
+                tc::fence_after_sync();
+                uint32_t s[BN];
+#pragma unroll
+                for (int c = 0; c < BN; c += 32) tc::tmem_ld32(t_s + c, s + c);
+                tc::tmem_wait_ld();
+                float c = a.scale_log2;
+                if (!(c > 0.f)) {   // the largest product is not the largest score: scores are scaled first
+#pragma unroll
+                    for (int i = 0; i < BN; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * c);
+                    c = 1.f;
+                }
+                if (limit < BN) {
+#pragma unroll
+                    for (int i = 0; i < BN; ++i)
+                        if (i >= limit) s[i] = 0xff800000u;
+                }
+                float top;
+                {   // four independent chains
+                    float t4[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        t4[q] = max3_nan(__uint_as_float(s[32 * q]), __uint_as_float(s[32 * q + 1]), __uint_as_float(s[32 * q + 2]));
+#pragma unroll
+                        for (int i = 3; i < 31; i += 2) t4[q] = max3_nan(t4[q], __uint_as_float(s[32 * q + i]), __uint_as_float(s[32 * q + i + 1]));
+                    }
+                    t4[0] = max3_nan(t4[0], t4[1], __uint_as_float(s[31]));
+                    t4[2] = max3_nan(t4[2], t4[3], __uint_as_float(s[63]));
+                    top = max3_nan(max3_nan(t4[0], t4[2], __uint_as_float(s[95])), __uint_as_float(s[127]), -INFINITY) * c;
+                }
+                const bool raise = !(top <= m + kRaise);   // (also where top is not a number)
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float f = raise ? exp2f(m - top) : 1.f;
+                    if (raise) m = top;
+                    l *= f;
+                    if (j > 0) {   // the accumulator is at rest once the group's last P V is done; the next is issued behind this tile's P
+                        if (!(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->o_done[x]), (od_base + (uint32_t)(j - 1)) & 1u, abort_flag)))) break;
+                        tc::fence_after_sync();
+#pragma unroll 1
+                        for (int cc = 0; cc < D; cc += 8) {
+                            uint32_t o[8];
+                            tc::tmem_ld8(t_o + cc, o);
+                            tc::tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tc::tmem_st8(t_o + cc, o);
+                        }
+                    }
+                }
+                const float from = m == -INFINITY ? 0.f : m;
+                const float2 c2 = make_float2(c, c), neg = make_float2(-from, -from);
+                float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+                for (int cc = 0; cc < 8; ++cc) {
+                    uint32_t pk[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float2 u = tc::ffma2(make_float2(__uint_as_float(s[cc * 16 + 2 * i]), __uint_as_float(s[cc * 16 + 2 * i + 1])), c2, neg);
+                        const float2 e = make_float2(fast_exp2(u.x), fast_exp2(u.y));
+                        if (i & 1)
+                            sum1 = tc::fadd2(sum1, e);
+                        else
+                            sum0 = tc::fadd2(sum0, e);
+                        pk[i] = pack2<T>(e.x, e.y);
+                    }
+                    tc::tmem_st8(t_s + kPColumn + cc * 8, pk);
+                }
+                l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+                tc::tmem_wait_st();
+                tc::fence_before_sync();
+                tc::mbar_arrive(bar(bars->p_full[buf]));
+            }
+            if (ok && !job.pair && x == 1) {
+                // single, group B: this row's (maximum, sum); O_B stays in tensor memory until group A has read it
+                xch[row] = make_float2(m, l);
+                tc::fence_before_sync();
+                tc::mbar_arrive(bar(bars->x_full));
+                ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->x_done), singles & 1u, abort_flag));
+            } else if (ok) {
+                ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->o_final), (uint32_t)jobs & 1u, abort_flag));
+                if (ok && !job.pair) ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->x_full), singles & 1u, abort_flag));
+                if (!ok) break;
+                tc::fence_after_sync();
+                float fa = 1.f, fb = 0.f;
+                if (!job.pair) {   // both groups' sums: O = O_A 2^(m_A - m) + O_B 2^(m_B - m)
+                    const float2 pb = xch[row];
+                    const float mm = fmaxf(m, pb.x);
+                    fa = m == -INFINITY ? 0.f : exp2f(m - mm);
+                    fb = pb.x == -INFINITY ? 0.f : exp2f(pb.x - mm);
+                    if (m != m || pb.x != pb.x) fa = fb = __int_as_float(0x7fc00000);
+                    l = l * fa + pb.y * fb;
+                    m = mm;
+                }
+                const int part = x == 0 ? job.part : job.part2;
+                if (part < 0) {
+                    const float inv = m == -INFINITY ? 0.f : 1.f / l;
+                    fa *= inv;
+                    fb *= inv;
+                }
+                T* out = static_cast<T*>(a.out) + (int64_t)(seg.token0 + token) * a.out_token + (int64_t)head * a.out_head;
+                float* to = a.partial + (int64_t)part * (kPartUnit * (D + 2));
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    tc::tmem_ld32(t_o + c, o);
+                    tc::tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fa);
+                    if (!job.pair) {
+                        uint32_t ob[32];
+                        tc::tmem_ld32(t_o + D + c, ob);   // O_B lies behind O_A
+                        tc::tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(fmaf(__uint_as_float(ob[i]), fb, __uint_as_float(o[i])));
+                    }
+                    if (!exists) continue;
+                    if (part < 0) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) w[e] = pack2<T>(__uint_as_float(o[8 * i + 2 * e]), __uint_as_float(o[8 * i + 2 * e + 1]));
+                            *reinterpret_cast<uint4*>(out + c + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            __stcg(reinterpret_cast<float4*>(to + (int64_t)row * D + c + 4 * i),
+                                   make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3])));
+                    }
+                }
+                if (exists && part >= 0) __stcg(reinterpret_cast<float2*>(to + BM * D + 2 * row), make_float2(m, l));
+                if (!job.pair) {
+                    tc::fence_before_sync();
+                    tc::mbar_arrive(bar(bars->x_done));
+                }
+            }
+            od_base += (uint32_t)n_own;
+            if (!job.pair) ++singles;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sp_base[b] += uses<NB>(n_score, b);
+        }
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    if (warp == 1) tc::tmem_dealloc(tmem, kTmemColumns);
+    if (tid == 0 && bars->abort_flag) atomicCAS(a.status, kDevOk, kDevTimeoutCache);
+}
+
+template <typename T, int D>
+cudaError_t wide_of(const CUtensorMap (&maps)[3], const CacheArgs& a, int ctas, cudaStream_t stream) {
+    return launch_kernel(cache_wide_kernel<T, D>, ctas, kThreads, Shape<D>::SMEM, stream, maps[0], maps[1], maps[2], a);
+}
+template <typename T, int D>
+cudaError_t allow() {
+    return cudaFuncSetAttribute(cache_wide_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::SMEM);
+}
+
+}  // namespace
+
+cudaError_t configure_cache_wide() {
+    cudaError_t e = allow<__nv_bfloat16, 64>();
+    if (e == cudaSuccess) e = allow<__nv_bfloat16, 128>();
+    if (e == cudaSuccess) e = allow<__half, 64>();
+    if (e == cudaSuccess) e = allow<__half, 128>();
+    return e;
+}
+
+// Returns cudaErrorInvalidValue if a tensor map cannot be encoded.
+cudaError_t launch_cache_wide(const CacheArgs& a, int head_dim, int dtype, int64_t n_pages, int ctas, cudaStream_t stream) {
+    const bool half = dtype == HTTM_FP16;
+    CUtensorMap maps[3];
+    const int page = 1 << a.page_shift, box = page < kWideKeys ? page : kWideKeys, per = kWideRows / a.group;
+    // a dimension of one element has no meaningful stride; any multiple of 16 bytes does
+    const int64_t q_head = a.kv_heads * a.group > 1 ? a.q_head : head_dim, q_token = a.n_tokens > 1 ? a.q_token : head_dim;
+    bool ok = encode_tensor_map_4d(&maps[0], half, a.q, Sizes4{{head_dim, a.group, a.n_tokens, a.kv_heads}}, Strides3{{q_head, q_token, q_head * a.group}},
+                                   Sizes4{{64, a.group, per, 1}});
+    const void* pools[2] = {a.k, a.v};
+    const int64_t strides[2][3] = {{a.k_slot, a.k_head, a.k_page}, {a.v_slot, a.v_head, a.v_page}};
+    for (int i = 0; i < 2; ++i)
+        ok = ok && encode_tensor_map_4d(&maps[1 + i], half, pools[i], Sizes4{{head_dim, page, a.kv_heads, n_pages}},
+                                        Strides3{{strides[i][0], a.kv_heads > 1 ? strides[i][1] : head_dim, n_pages > 1 ? strides[i][2] : head_dim}},
+                                        Sizes4{{64, box, 1, 1}});
+    if (!ok) return cudaErrorInvalidValue;
+    if (half) return head_dim == 64 ? wide_of<__half, 64>(maps, a, ctas, stream) : wide_of<__half, 128>(maps, a, ctas, stream);
+    return head_dim == 64 ? wide_of<__nv_bfloat16, 64>(maps, a, ctas, stream) : wide_of<__nv_bfloat16, 128>(maps, a, ctas, stream);
+}
+
+}  // namespace httm

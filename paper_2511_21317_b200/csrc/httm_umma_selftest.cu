@@ -44,6 +44,19 @@ bool encode_rows_tensor_map(CUtensorMap* map, const void* base, int64_t rows, in
     return r == CUDA_SUCCESS;
 }
 
+bool encode_tensor_map_4d(CUtensorMap* map, bool fp16, const void* base, const Sizes4& dims, const Strides3& strides, const Sizes4& box) {
+    std::call_once(g_encode_once, resolve_encode);
+    if (!g_encode) return false;
+    cuuint64_t d[4], st[3];
+    cuuint32_t b[4];
+    const cuuint32_t elem[4] = {1, 1, 1, 1};
+    for (int i = 0; i < 4; ++i) d[i] = (cuuint64_t)dims.v[i], b[i] = (cuuint32_t)box.v[i];
+    for (int i = 0; i < 3; ++i) st[i] = (cuuint64_t)strides.v[i] * 2;
+    return g_encode(map, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), d, st, b, elem,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool encode_patch_tensor_map(CUtensorMap* map, const void* base, int grid_w, int grid_h, int frames, int64_t heads,
                              int64_t stride_token, int64_t tokens_per_frame, int64_t stride_head, int box_w, int box_h,
                              int box_frames) {

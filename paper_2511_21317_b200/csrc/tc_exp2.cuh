@@ -1,0 +1,36 @@
+// 2^t for the weights of a softmax: on the special-function unit, and for two values at a time without it.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include "tc_sm100.cuh"
+
+namespace httm {
+
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// 2^t for two values without the special-function unit.  The argument is clamped to [-125, 125] (an argument of 125 or more gives
+// 2^125, which the caller's test of the tile's row sum catches; without the clamp the exponent arithmetic below would wrap) by a saturating
+// multiply-add, u = t / 250 + 1 / 2: min / max clamps took another 8 cycles of the ALU.  Then round-to-nearest range reduction
+// t = n + f, f in [-0.5, 0.5] (the integer lands in the low mantissa bits of t + 1.5 * 2^23), a cubic minimax polynomial for
+// 2^f (relative error < 1e-4, far below the bf16 rounding of P) evaluated with packed fp32 FMAs, and n added to the exponent
+// field.  t itself is s c - m in one rounding, as the other exponentials take it: u straight from the score, s (c / 250) +
+// (125 - m) / 250, rounds two constants in proportion to m, which weighed these keys against the others by 1e-3 at scores of
+// 3e4 (error of the output against 64 bits 5.65e-3 instead of 5.61e-3 there, 7.28e-2 instead of 7.14e-2 at 5e5).
+__device__ __forceinline__ float2 exp2_poly2(float2 t) {
+    const float kMagic = 12582912.0f - 125.0f;
+    const float2 magic = make_float2(kMagic, kMagic), width = make_float2(250.0f, 250.0f);
+    const float2 u = make_float2(tc::ffma_sat(t.x, 1.0f / 250.0f, 0.5f), tc::ffma_sat(t.y, 1.0f / 250.0f, 0.5f));
+    const float2 tt = tc::ffma2(u, width, magic);
+    const float2 f = tc::ffma2(u, width, tc::fsub2(magic, tt));
+    float2 q = tc::ffma2(make_float2(0.055171460f, 0.055171460f), f, make_float2(0.24261086f, 0.24261086f));
+    q = tc::ffma2(q, f, make_float2(0.69326097f, 0.69326097f));
+    q = tc::ffma2(q, f, make_float2(0.99992812f, 0.99992812f));
+    return make_float2(__int_as_float(__float_as_int(q.x) + (__float_as_int(tt.x) << 23)),
+                       __int_as_float(__float_as_int(q.y) + (__float_as_int(tt.y) << 23)));
+}
+}  // namespace httm

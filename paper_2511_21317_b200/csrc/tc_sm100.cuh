@@ -289,4 +289,13 @@ bool encode_patch_tensor_map(CUtensorMap* map, const void* base, int grid_w, int
 bool encode_frame_tensor_map(CUtensorMap* map, const void* base, int64_t tokens_per_frame, int frames, int64_t heads,
                              int64_t stride_token, int64_t stride_head, int box_tokens);
 
+// Host: 4-D map of 16-bit elements (bf16, or fp16), strides of dimensions 1 .. 3 in elements, 128-byte swizzle (the box is 64 elements wide).
+struct Sizes4 {
+    int64_t v[4];
+};
+struct Strides3 {
+    int64_t v[3];
+};
+bool encode_tensor_map_4d(CUtensorMap* map, bool fp16, const void* base, const Sizes4& dims, const Strides3& strides, const Sizes4& box);
+
 }  // namespace httm

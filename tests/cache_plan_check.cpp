@@ -24,7 +24,7 @@ static int pick(int lo, int hi) { return std::uniform_int_distribution<int>(lo, 
 
 static bool one_round() {
     httm_batch_config c{};
-    const int groups[] = {1, 1, 2, 3, 4, 5, 8, 16, 17, 33, 40, 64};
+    const int groups[] = {1, 1, 2, 3, 4, 5, 8, 16, 17, 40, 65, 128};
     c.kv_heads = pick(1, 8);
     const int group = groups[pick(0, 11)];
     c.heads = c.kv_heads * group;

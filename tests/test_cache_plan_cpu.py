@@ -56,7 +56,7 @@ def test_rotary_refuses(kw, code):
     assert e.value.code == code
 
 
-@pytest.mark.parametrize("kw,code", [(dict(heads=6, kv_heads=4), -1), (dict(heads=65, kv_heads=1), -2), (dict(head_dim=96), -2), (dict(page_size=24), -2),
+@pytest.mark.parametrize("kw,code", [(dict(heads=6, kv_heads=4), -1), (dict(heads=129, kv_heads=1), -2), (dict(head_dim=96), -2), (dict(page_size=24), -2),
                                      (dict(page_size=8), -2), (dict(n_pages=0), -1), (dict(n_pages=1 << 30), -1), (dict(kv_heads=0), -1), (dict(device=99), -1)])
 def test_batch_refuses(kw, code):
     from paper_2511_21317_b200 import binding, kv_cache as kc
