@@ -252,8 +252,7 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
     a.job_start = part_of<int32_t>(b, b->at.narrow_start);
     a.table = part_of<int32_t>(b, b->at.table);
     a.parts = part_of<int2>(b, b->at.parts);
-    a.prefix_seg = part_of<int32_t>(b, b->at.prefix_seg);
-    a.own_seg = part_of<int32_t>(b, b->at.own_seg);
+    a.combine_tasks = part_of<CombineTask>(b, b->at.combine_tasks);
     a.q = q.ptr, a.k = k_pages.ptr, a.v = v_pages.ptr, a.out = out.ptr;
     a.q_head = q.stride_head, a.q_token = q.stride_token, a.out_head = out.stride_head, a.out_token = out.stride_token;
     a.k_page = k_pages.stride_page, a.k_head = k_pages.stride_head, a.k_slot = k_pages.stride_slot;
@@ -273,7 +272,8 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
         rc = cuda_result(launch_cache_wide(w, c.head_dim, dtype, c.n_pages, (int)p.wide_start.size() - 1, stream), "cache_attention launch");
     }
     if (!rc && !p.narrow_jobs.empty()) rc = cuda_result(launch_cache_narrow(a, c.head_dim, dtype, (int)p.narrow_start.size() - 1, stream), "cache_attention launch");
-    if (!rc && p.combine) rc = cuda_result(launch_cache_combine(a, c.head_dim, dtype, stream), "cache_attention launch");
+    if (!rc && !p.combine_tasks.empty())
+        rc = cuda_result(launch_cache_combine(a, c.head_dim, dtype, (int)p.combine_tasks.size(), stream), "cache_attention launch");
     return rc;
 }
 

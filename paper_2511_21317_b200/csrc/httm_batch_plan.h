@@ -26,12 +26,13 @@ struct BatchInput {
 struct BatchPlan {
     int32_t n_tokens = 0, page_shift = 0, part_units = 0;
     int64_t last_position = -1;       // largest place of a new token behind the prefix
-    bool can_append = true, same_place = false, combine = false;
+    bool can_append = true, same_place = false;
     std::vector<CacheSeg> segs;
     std::vector<CacheJob> narrow_jobs, wide_jobs;
     std::vector<int32_t> narrow_start, wide_start;   // [CTAs + 1]
     std::vector<int32_t> table, prefix_seg, own_seg, slots, positions;
     std::vector<int2> parts;   // [row tile][kv head]
+    std::vector<CombineTask> combine_tasks;
 };
 
 inline int32_t pages_of(int32_t length, int32_t page) { return (int32_t)(((int64_t)length + page - 1) / page); }
@@ -105,9 +106,10 @@ struct Dealer {
     void deal(const std::vector<BatchItem>& items, const std::vector<char>& sole, int ctas, int job_cost, int least) {
         of.assign(ctas, {});
         if (items.empty()) return;
-        double total = 0;
-        for (const BatchItem& it : items) total += it.tiles * it.cost + job_cost;
-        double quota = std::max(total / ctas, least * items[0].cost + job_cost);
+        // What every CTA should have to do if each also gets one job that is cut off.
+        double total = 0, most = 0;
+        for (const BatchItem& it : items) total += it.tiles * it.cost + job_cost, most = std::max(most, it.cost);
+        const double fair = std::max(total / ctas + job_cost, least * most + job_cost);
         std::vector<double> load(ctas, 0.0);
         std::priority_queue<std::pair<double, int>, std::vector<std::pair<double, int>>, std::greater<std::pair<double, int>>> idle;
         for (int c = 0; c < ctas; ++c) idle.push({0.0, c});
@@ -115,37 +117,49 @@ struct Dealer {
         std::vector<std::pair<BatchItem, int>> whole;
         for (const BatchItem& it : items) {
             const auto top = idle.top();
-            if (top.first + it.tiles * it.cost + job_cost <= quota + 0.5 * least * it.cost) {
+            const double then = top.first + it.tiles * it.cost + job_cost;
+            if (then <= fair) {
                 idle.pop();
                 whole.push_back({it, top.second});
-                load[top.second] += it.tiles * it.cost + job_cost;
-                idle.push({load[top.second], top.second});
+                load[top.second] = then;
+                idle.push({then, top.second});
             } else {
                 left.push_back(it);
             }
         }
+        // The rest is cut where a CTA is full; what full means is found by bisection (the smallest load with which everything has a place).
         struct Piece {
             BatchItem it;
             int cta, t0, t1;
         };
         std::vector<Piece> pieces;
-        size_t next = 0;
-        int done = 0;   // key tiles of left[next] that are dealt
-        while (next < left.size()) {
+        auto cut = [&](double full, bool keep) {
+            size_t next = 0;
+            int done = 0;   // key tiles of left[next] that are dealt
             for (int c = 0; c < ctas && next < left.size(); ++c) {
+                double at = load[c];
                 while (next < left.size()) {
-                    const int rest = left[next].tiles - done;
-                    const double room = quota - load[c] - job_cost;
-                    int n = room <= 0 ? 0 : (int)std::min((double)rest, std::ceil(room / left[next].cost));
-                    if (n < rest && rest - n < least) n = rest - n <= least / 2 ? rest : n;   // no crumbs
-                    if (n < std::min(least, rest)) break;
-                    pieces.push_back({left[next], c, done, done + n});
-                    load[c] += n * left[next].cost + job_cost;
+                    const BatchItem& it = left[next];
+                    const int rest = it.tiles - done;
+                    const double room = (full - at - job_cost) / it.cost;
+                    const int n = room >= rest ? rest : (int)std::max(0.0, std::floor(room + 1e-9));
+                    if (n == 0 || (n < rest && n < least)) break;
+                    if (keep) pieces.push_back({it, c, done, done + n});
+                    at += n * it.cost + job_cost;
                     done += n;
-                    if (done == left[next].tiles) ++next, done = 0;
+                    if (done == it.tiles) ++next, done = 0;
                 }
             }
-            quota += std::max(1.0, 0.02 * quota);
+            return next == left.size();
+        };
+        if (!left.empty()) {
+            double lo = 0, hi = fair;
+            while (!cut(hi, false)) lo = hi, hi *= 2;
+            for (int i = 0; i < 12; ++i) {
+                const double mid = 0.5 * (lo + hi);
+                (cut(mid, false) ? hi : lo) = mid;
+            }
+            cut(hi, true);
         }
         // parts of one row tile and head lie side by side: count them first
         std::vector<int> count((size_t)p->segs.size() * kv_heads, 0);
@@ -162,12 +176,12 @@ struct Dealer {
         };
         for (const auto& w : whole) {
             const bool direct = sole[w.first.seg];
-            if (!direct) place(w.first), p->combine = true;
+            if (!direct) place(w.first);
             take(w.second, w.first, 0, w.first.tiles, direct);
         }
         for (const Piece& q : pieces) {
             const bool direct = sole[q.it.seg] && q.t0 == 0 && q.t1 == q.it.tiles;
-            if (!direct) place(q.it), p->combine = true;
+            if (!direct) place(q.it);
             take(q.cta, q.it, q.t0, q.t1, direct);
         }
     }
@@ -265,7 +279,6 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     for (int32_t t = 0; t < p->n_tokens; ++t) {
         const int32_t a = p->prefix_seg[t], b = p->own_seg[t];
         if (a >= 0 && b >= 0) sole[a] = sole[b] = 0;
-        if (a < 0 && b < 0) p->combine = true;   // (it writes the zeros of rows without keys)
     }
     p->parts.assign(p->segs.size() * c.kv_heads, int2{-1, 0});
     // Two row tiles of 128 rows form a pair if they look at the same keys (a pair walks those of the second one, which sees at least as many) and are dealt
@@ -291,12 +304,23 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     d.collect(&p->wide_jobs, &p->wide_start);
     d.deal(narrow, sole, 2 * sm_count, 2, 4);
     d.collect(&p->narrow_jobs, &p->narrow_start);
+    // rows whose keys were cut or lie in two row tiles; rows that see no key (they get zeros)
+    const int per_task = std::max(1, kCombineRows / group);
+    for (int32_t t = 0; t < p->n_tokens;) {
+        const int32_t a = p->prefix_seg[t], b = p->own_seg[t];
+        int32_t n = 1;
+        while (n < per_task && t + n < p->n_tokens && p->prefix_seg[t + n] == a && p->own_seg[t + n] == b) ++n;
+        for (int h = 0; h < c.kv_heads; ++h) {
+            auto direct = [&](int32_t s) { return s >= 0 && p->parts[(size_t)s * c.kv_heads + h].y < 0; };
+            if (!direct(a) && !direct(b)) p->combine_tasks.push_back(CombineTask{t, n, a, b, h, {0, 0, 0}});
+        }
+        t += n;
+    }
 }
 
 // Where the parts of a plan lie in one block (offsets in bytes, multiples of 256).
 struct BatchLayout {
-    size_t segs = 0, narrow_jobs = 0, wide_jobs = 0, narrow_start = 0, wide_start = 0, table = 0, parts = 0, prefix_seg = 0, own_seg = 0, slots = 0, positions = 0,
-           bytes = 0;
+    size_t segs = 0, narrow_jobs = 0, wide_jobs = 0, narrow_start = 0, wide_start = 0, table = 0, parts = 0, combine_tasks = 0, slots = 0, positions = 0, bytes = 0;
     BatchLayout() = default;
     explicit BatchLayout(const BatchPlan& p) {
         auto room = [&](size_t n) {
@@ -306,7 +330,7 @@ struct BatchLayout {
         };
         auto of = [&](const auto& v) { return room(v.size() * sizeof(v[0])); };
         segs = of(p.segs), narrow_jobs = of(p.narrow_jobs), wide_jobs = of(p.wide_jobs), narrow_start = of(p.narrow_start), wide_start = of(p.wide_start);
-        table = of(p.table), parts = of(p.parts), prefix_seg = of(p.prefix_seg), own_seg = of(p.own_seg), slots = of(p.slots), positions = of(p.positions);
+        table = of(p.table), parts = of(p.parts), combine_tasks = of(p.combine_tasks), slots = of(p.slots), positions = of(p.positions);
         bytes += 256;
     }
     void write(const BatchPlan& p, unsigned char* to) const {
@@ -314,7 +338,7 @@ struct BatchLayout {
             if (!v.empty()) memcpy(to + at, v.data(), v.size() * sizeof(v[0]));
         };
         put(segs, p.segs), put(narrow_jobs, p.narrow_jobs), put(wide_jobs, p.wide_jobs), put(narrow_start, p.narrow_start), put(wide_start, p.wide_start);
-        put(table, p.table), put(parts, p.parts), put(prefix_seg, p.prefix_seg), put(own_seg, p.own_seg), put(slots, p.slots), put(positions, p.positions);
+        put(table, p.table), put(parts, p.parts), put(combine_tasks, p.combine_tasks), put(slots, p.slots), put(positions, p.positions);
     }
 };
 

@@ -113,13 +113,20 @@ struct alignas(16) CacheJob {   // key tiles [tile0, tile1) of a row tile: those
     int32_t part2;              // of the second row tile
     int32_t pad;
 };
+constexpr int kCombineRows = 8;
+struct alignas(16) CombineTask {   // rows of a few tokens and one key head whose partial results are to be added up
+    int32_t token0, tokens;
+    int32_t prefix_seg, own_seg;   // the row tiles that hold them, or -1
+    int32_t head;
+    int32_t pad[3];
+};
 struct CacheArgs {
     const CacheSeg* segs;
     const CacheJob* jobs;
     const int32_t* job_start;   // [CTAs + 1]
     const int32_t* table;       // pages of the prefix, then of every sequence
     const int2* parts;          // [row tile][kv head]: first unit, number of partial results (-1: written by its job)
-    const int32_t *prefix_seg, *own_seg;   // [token]: the row tiles that hold it, or -1
+    const CombineTask* combine_tasks;
     const void *q, *k, *v;
     void* out;
     int64_t q_head, q_token, out_head, out_token;
@@ -133,6 +140,6 @@ cudaError_t configure_cache_attention();
 cudaError_t launch_cache_narrow(const CacheArgs& a, int head_dim, int dtype, int ctas, cudaStream_t stream);
 cudaError_t configure_cache_wide();
 cudaError_t launch_cache_wide(const CacheArgs& a, int head_dim, int dtype, int64_t n_pages, int ctas, cudaStream_t stream);
-cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, cudaStream_t stream);
+cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, int tasks, cudaStream_t stream);
 
 }  // namespace httm

@@ -281,72 +281,118 @@ __global__ void __launch_bounds__(kThreads) cache_narrow_kernel(const __grid_con
     }
 }
 
-// The partial results of every row whose keys were shared out, added up in the order of the keys; a row without any gets zeros.
-// One warp per row; the results are in L2.
+// The partial results of rows whose keys were shared out, added up in the order of the keys: out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m).  A CTA takes a few
+// rows; with fewer rows than warps the parts of a row are dealt to several warps, since a row of single tokens behind a long prefix has some
+// twenty parts and the time is that of the loads behind one another.  A row without parts gets zeros.
 constexpr int kCombineWarps = 8;
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const __grid_constant__ CacheArgs a) {
     constexpr int V = D / 32;   // channels of a lane
+    __shared__ float4 shared_sum[kCombineWarps][32];
+    __shared__ float2 shared_stat[kCombineWarps];
     depend_wait();
     dependents_launch();
-    const int heads = a.kv_heads * a.group, lane = threadIdx.x & 31;
-    const int64_t row_id = (int64_t)blockIdx.x * kCombineWarps + (threadIdx.x >> 5);
-    if (row_id >= (int64_t)a.n_tokens * heads) return;
-    const int token = (int)(row_id / heads), head = (int)(row_id - (int64_t)token * heads), kv = head / a.group;
-    const int segs[2] = {ld_global(a.prefix_seg + token), ld_global(a.own_seg + token)};
-    const float *from[2], *stat[2];
-    int n[2] = {0, 0};
-    int64_t stride[2];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const CombineTask task = a.combine_tasks[blockIdx.x];
+    const int rows = task.tokens * a.group;
+    int ways = 1;   // warps that share a row's parts
+    while (2 * ways * rows <= kCombineWarps) ways *= 2;
+    const int way = warp % ways;
+    // the parts of a tile lie one behind the other: n, the tile's rows, its first row of this task
+    int n0 = 0, n1 = 0, rows0 = 0, rows1 = 0, first0 = 0, first1 = 0;
+    const float *base0 = nullptr, *base1 = nullptr;
+    auto find = [&](int seg, int& n, int& tile_rows, int& first, const float*& base) {
+        if (seg < 0) return;
+        const int2 part = a.parts[(int64_t)seg * a.kv_heads + task.head];
+        const int4 s = *reinterpret_cast<const int4*>(a.segs + seg);   // token0, tokens, tile_rows
+        n = part.y;
+        tile_rows = s.z;
+        first = (task.token0 - s.x) * a.group;
+        base = a.partial + (int64_t)part.x * (kPartUnit * (D + 2));
+    };
+    find(task.prefix_seg, n0, rows0, first0, base0);
+    find(task.own_seg, n1, rows1, first1, base1);
+    const int n = n0 + n1;
+    for (int r0 = 0; r0 < rows; r0 += kCombineWarps / ways) {
+        const int row = r0 + warp / ways;
+        const bool here = row < rows;
+        // part p of the row: its values and its (maximum, sum)
+        auto values = [&](int p) {
+            return p < n0 ? base0 + (int64_t)p * rows0 * (D + 2) + (first0 + row) * D : base1 + (int64_t)(p - n0) * rows1 * (D + 2) + (first1 + row) * D;
+        };
+        auto stat = [&](int p) {
+            return p < n0 ? base0 + (int64_t)p * rows0 * (D + 2) + rows0 * D + 2 * (first0 + row)
+                          : base1 + (int64_t)(p - n0) * rows1 * (D + 2) + rows1 * D + 2 * (first1 + row);
+        };
+        float top = -INFINITY, total = 0.f, sum[V];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (segs[i] < 0) continue;
-        const int2 part = a.parts[(int64_t)segs[i] * a.kv_heads + kv];
-        if (part.y < 0) return;   // its job has written the row
-        const CacheSeg& seg = a.segs[segs[i]];
-        const int row = (token - seg.token0) * a.group + head % a.group;
-        n[i] = part.y;
-        stride[i] = (int64_t)seg.tile_rows * (D + 2);
-        const float* base = a.partial + (int64_t)part.x * (kPartUnit * (D + 2));
-        from[i] = base + row * D + lane * V;
-        stat[i] = base + seg.tile_rows * D + 2 * row;
-    }
-    float top = -INFINITY;
+        for (int c = 0; c < V; ++c) sum[c] = 0.f;
+        if (here) {
+            for (int p0 = way; p0 < n; p0 += 32 * ways) {   // 32 parts at a time, one per lane
+                const int mine = p0 + lane * ways;
+                float2 st = make_float2(-INFINITY, 0.f);
+                if (mine < n) st = __ldcg(reinterpret_cast<const float2*>(stat(mine)));
+                float high = st.x;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        for (int p = lane; p < n[i]; p += 32) top = fmaxf(top, __ldcg(stat[i] + p * stride[i]));
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float sum[V], total = 0.f;
+                for (int o = 16; o > 0; o >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+                const float to = fmaxf(top, high), shrink = top == -INFINITY ? 0.f : exp2_fast(top - to);
+                const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - to);
+                top = to;
+                total = fmaf(st.y, f, total * shrink);   // (a lane's share; added up below)
 #pragma unroll
-    for (int c = 0; c < V; ++c) sum[c] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        for (int p0 = 0; p0 < n[i]; p0 += 32) {
-            float2 st = make_float2(-INFINITY, 0.f);
-            if (p0 + lane < n[i]) st = __ldcg(reinterpret_cast<const float2*>(stat[i] + (p0 + lane) * stride[i]));
-            const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - top);
-            total = fmaf(st.y, f, total);
-            const int m = min(32, n[i] - p0);
-#pragma unroll 4
-            for (int p = 0; p < m; ++p) {
-                const float w = __shfl_sync(0xffffffffu, f, p);
-                const float* at = from[i] + (p0 + p) * stride[i];
-                if constexpr (V == 4) {
-                    const float4 v = __ldcg(reinterpret_cast<const float4*>(at));
-                    sum[0] = fmaf(v.x, w, sum[0]), sum[1] = fmaf(v.y, w, sum[1]), sum[2] = fmaf(v.z, w, sum[2]), sum[3] = fmaf(v.w, w, sum[3]);
-                } else {
-                    const float2 v = __ldcg(reinterpret_cast<const float2*>(at));
-                    sum[0] = fmaf(v.x, w, sum[0]), sum[1] = fmaf(v.y, w, sum[1]);
+                for (int c = 0; c < V; ++c) sum[c] *= shrink;
+                const int m = min(32, (n - p0 + ways - 1) / ways);
+#pragma unroll 8
+                for (int i = 0; i < m; ++i) {
+                    const float w = __shfl_sync(0xffffffffu, f, i);
+                    const float* at = values(p0 + i * ways) + lane * V;
+                    if constexpr (V == 4) {
+                        const float4 v = __ldcg(reinterpret_cast<const float4*>(at));
+                        sum[0] = fmaf(v.x, w, sum[0]), sum[1] = fmaf(v.y, w, sum[1]), sum[2] = fmaf(v.z, w, sum[2]), sum[3] = fmaf(v.w, w, sum[3]);
+                    } else {
+                        const float2 v = __ldcg(reinterpret_cast<const float2*>(at));
+                        sum[0] = fmaf(v.x, w, sum[0]), sum[1] = fmaf(v.y, w, sum[1]);
+                    }
                 }
             }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        }
+        if (ways > 1) {   // (one round of rows: rows * ways <= warps)
+            if constexpr (V == 4)
+                shared_sum[warp][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            else
+                shared_sum[warp][lane] = make_float4(sum[0], sum[1], 0.f, 0.f);
+            if (lane == 0) shared_stat[warp] = make_float2(top, total);
+            __syncthreads();
+            if (way == 0) {
+                float high = top;
+                for (int i = 1; i < ways; ++i) high = fmaxf(high, shared_stat[warp + i].x);
+                const float own = top == -INFINITY ? 0.f : exp2_fast(top - high);
+                total *= own;
+#pragma unroll
+                for (int c = 0; c < V; ++c) sum[c] *= own;
+                for (int i = 1; i < ways; ++i) {
+                    const float2 st = shared_stat[warp + i];
+                    const float4 v = shared_sum[warp + i][lane];
+                    const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - high);
+                    total = fmaf(st.y, f, total);
+                    sum[0] = fmaf(v.x, f, sum[0]), sum[1] = fmaf(v.y, f, sum[1]);
+                    if constexpr (V == 4) sum[2] = fmaf(v.z, f, sum[2]), sum[3] = fmaf(v.w, f, sum[3]);
+                }
+                top = high;
+            }
+        }
+        if (here && way == 0) {
+            const float inv = top == -INFINITY ? 0.f : 1.f / total;
+            const int token = task.token0 + row / a.group, head = task.head * a.group + row % a.group;
+            T* out = static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + lane * V;
+            if constexpr (V == 4)
+                *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum[0] * inv, sum[1] * inv), pack2<T>(sum[2] * inv, sum[3] * inv));
+            else
+                *reinterpret_cast<uint32_t*>(out) = pack2<T>(sum[0] * inv, sum[1] * inv);
         }
     }
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    const float inv = top == -INFINITY ? 0.f : 1.f / total;
-    T* out = static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + lane * V;
-    if constexpr (V == 4)
-        *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum[0] * inv, sum[1] * inv), pack2<T>(sum[2] * inv, sum[3] * inv));
-    else
-        *reinterpret_cast<uint32_t*>(out) = pack2<T>(sum[0] * inv, sum[1] * inv);
 }
 
 template <typename F>
@@ -358,9 +404,8 @@ cudaError_t narrow_of(const CacheArgs& a, int ctas, cudaStream_t stream) {
     return launch_kernel(cache_narrow_kernel<T, D>, ctas, kThreads, kStages * kStageBytes<D>, stream, a);
 }
 template <typename T, int D>
-cudaError_t combine_of(const CacheArgs& a, cudaStream_t stream) {
-    const int64_t rows = (int64_t)a.n_tokens * a.kv_heads * a.group;
-    return launch_kernel(cache_combine_kernel<T, D>, (unsigned)((rows + kCombineWarps - 1) / kCombineWarps), 32 * kCombineWarps, 0, stream, a);
+cudaError_t combine_of(const CacheArgs& a, int tasks, cudaStream_t stream) {
+    return launch_kernel(cache_combine_kernel<T, D>, tasks, 32 * kCombineWarps, 0, stream, a);
 }
 
 }  // namespace
@@ -377,9 +422,9 @@ cudaError_t launch_cache_narrow(const CacheArgs& a, int head_dim, int dtype, int
     if (dtype == HTTM_BF16) return head_dim == 64 ? narrow_of<__nv_bfloat16, 64>(a, ctas, stream) : narrow_of<__nv_bfloat16, 128>(a, ctas, stream);
     return head_dim == 64 ? narrow_of<__half, 64>(a, ctas, stream) : narrow_of<__half, 128>(a, ctas, stream);
 }
-cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, cudaStream_t stream) {
-    if (dtype == HTTM_BF16) return head_dim == 64 ? combine_of<__nv_bfloat16, 64>(a, stream) : combine_of<__nv_bfloat16, 128>(a, stream);
-    return head_dim == 64 ? combine_of<__half, 64>(a, stream) : combine_of<__half, 128>(a, stream);
+cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, int tasks, cudaStream_t stream) {
+    if (dtype == HTTM_BF16) return head_dim == 64 ? combine_of<__nv_bfloat16, 64>(a, tasks, stream) : combine_of<__nv_bfloat16, 128>(a, tasks, stream);
+    return head_dim == 64 ? combine_of<__half, 64>(a, tasks, stream) : combine_of<__half, 128>(a, tasks, stream);
 }
 
 }  // namespace httm

@@ -82,7 +82,6 @@ static bool one_round() {
                 }
             }
             NEED(own == sees && shared == prefix);
-            NEED(p.combine || (p.prefix_seg[t] >= 0) != (p.own_seg[t] >= 0));
             if (queries[i] <= lengths[i]) {
                 const int place = lengths[i] - queries[i] + j;
                 NEED(p.slots[t] == tables[(size_t)i * stride + place / c.page_size] * c.page_size + place % c.page_size);
@@ -133,7 +132,7 @@ static bool one_round() {
             // a pair walks the key tiles of its second row tile, which sees at least as many
             const int least = (seg.prefix_keys + keys - 1) / keys + (seg.own_keys + keys - 1) / keys;
             NEED(at >= least && (seg.tile_rows == kWideRows || at == least));
-            NEED(parts.y == -1 || (parts.y == n && n > 0 && p.combine));
+            NEED(parts.y == -1 || (parts.y == n && n > 0));
             if (parts.y > 0) ranges.insert({parts.x, end});
             if (parts.y < 0)
                 for (int k = seg.token0; k < seg.token0 + seg.tokens; ++k) NEED((p.prefix_seg[k] < 0) != (p.own_seg[k] < 0));
@@ -143,6 +142,22 @@ static bool one_round() {
         NEED(r.first >= last);
         last = r.second;
     }
+    // rows that are written by a job, and rows whose partial results are added up: every row exactly once
+    std::map<std::pair<int, int>, int> written;   // (token, head)
+    for (const CombineTask& k : p.combine_tasks) {
+        NEED(k.tokens > 0 && k.token0 >= 0 && k.token0 + k.tokens <= tokens && k.head >= 0 && k.head < c.kv_heads);
+        for (int i = k.token0; i < k.token0 + k.tokens; ++i) {
+            NEED(p.prefix_seg[i] == k.prefix_seg && p.own_seg[i] == k.own_seg);
+            ++written[{i, k.head}];
+        }
+        for (int which : {k.prefix_seg, k.own_seg}) NEED(which < 0 || p.parts[(size_t)which * c.kv_heads + k.head].y > 0);
+    }
+    for (int s = 0; s < (int)p.segs.size(); ++s)
+        for (int h = 0; h < c.kv_heads; ++h)
+            if (p.parts[(size_t)s * c.kv_heads + h].y < 0)
+                for (int i = p.segs[s].token0; i < p.segs[s].token0 + p.segs[s].tokens; ++i) ++written[{i, h}];
+    NEED((int64_t)written.size() == (int64_t)tokens * c.kv_heads);
+    for (const auto& w : written) NEED(w.second == 1);
     // the block of memory
     const BatchLayout at(p);
     std::vector<unsigned char> block(at.bytes, 0);
