@@ -3,11 +3,11 @@
 // One CTA per SM walks its jobs.  A job is a PAIR of row tiles (A, B) that share a stream of keys, or a SINGLE row tile whose even key tiles go to
 // softmax group A and whose odd ones go to group B (two softmaxes over disjoint keys, combined at the end).  Either way score tile k belongs to
 // group k mod 2 and lies in score buffer k mod NB of tensor memory:
-//   warp 0      producer: Q tiles once, then a ring of K and V tiles of 128 keys, page by page (TMA, 128-byte swizzle)
+//   warps 0, 10 producers: Q tiles once, then rings of K and of V tiles of 128 keys, page by page (TMA, 128-byte swizzle)
 //   warp 1      issues the products S = Q K^T (operands in shared memory) and O += P V (P in tensor memory over its S, V from shared memory)
 //   warps 2-5   softmax of group A, one thread per row: S from tensor memory, weights back as pairs of 16 bits; warps 6-9 of group B
 // S(k + NB) is issued right behind P(k) V into the buffer that this frees.  Tensor memory: NB score buffers of 128 columns and two accumulators of D, 512
-// columns in all (NB = 3 for 64 channels, 2 for 128; the ring has as many stages, 128 and 192 KB with the Q tiles).
+// columns in all (NB = 3 for 64 channels, 2 for 128).  Shared memory: two Q tiles and rings of 6 (2 for 128 channels) stages, 224 (192) KB.
 //
 // Q comes in boxes of (channels, heads of the group, tokens), so the rows of a tile are (token, head) whatever the group's size and the tensor's
 // strides; rows that a tile does not fill compute something that nobody stores.  Keys behind the end of the prefix or of a sequence are masked
@@ -28,7 +28,7 @@ namespace httm {
 namespace {
 
 constexpr int BM = kWideRows, BN = kWideKeys;
-constexpr int kThreads = 320;
+constexpr int kThreads = 352;   // registers are granted per four warps: as many per thread as with twelve
 constexpr int kTmemColumns = 512;
 constexpr int kSubTile = BM * 128;   // 128 rows of 64 channels
 constexpr int kPColumn = 64;         // P (16-bit pairs, 64 columns) lies over the last 64 columns of its S
@@ -36,16 +36,17 @@ constexpr float kRaise = 8.f;        // in units of log2
 
 template <int D>
 struct Shape {
-    static constexpr int NB = D == 64 ? 3 : 2;   // score buffers, and stages of the ring
-    static constexpr int SUB = D / 64;           // 64-channel parts of a tile
+    static constexpr int NB = D == 64 ? 3 : 2;    // score buffers
+    static constexpr int ST = D == 64 ? 6 : 2;    // stages of the rings of K and of V: NB, or 2 NB where there is room
+    static constexpr int SUB = D / 64;            // 64-channel parts of a tile
     static constexpr int TILE = SUB * kSubTile;
-    static constexpr int SMEM = (2 + 2 * NB) * TILE + 1024 /*alignment*/ + 512 /*barriers*/ + BM * 8 /*exchange*/;
+    static constexpr int SMEM = (2 + 2 * ST) * TILE + 1024 /*alignment*/ + 512 /*barriers*/ + BM * 8 /*exchange*/;
 };
 
-template <int NB>
+template <int NB, int ST>
 struct Barriers {
     uint64_t q_full, q_free;
-    uint64_t k_full[NB], k_empty[NB], v_full[NB], v_empty[NB];
+    uint64_t k_full[ST], k_empty[ST], v_full[ST], v_empty[ST];
     uint64_t v_tail;                 // a V tile that needs zeros has arrived
     uint64_t s_full[NB], p_full[NB];
     uint64_t o_done[2];              // one completion per P V of the group
@@ -101,12 +102,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ CacheArgs a) {
     using S = Shape<D>;
-    constexpr int NB = S::NB, SUB = S::SUB, TILE = S::TILE;
+    constexpr int NB = S::NB, ST = S::ST, SUB = S::SUB, TILE = S::TILE;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    const uint32_t s_q = tc::smem_addr(smem), s_k = s_q + 2 * TILE, s_v = s_k + NB * TILE;
-    Barriers<NB>* bars = reinterpret_cast<Barriers<NB>*>(smem + (2 + 2 * NB) * TILE);
-    static_assert(sizeof(Barriers<NB>) <= 512, "the barriers have 512 bytes");
+    const uint32_t s_q = tc::smem_addr(smem), s_k = s_q + 2 * TILE, s_v = s_k + ST * TILE;
+    using Bars = Barriers<NB, ST>;
+    Bars* bars = reinterpret_cast<Bars*>(smem + (2 + 2 * ST) * TILE);
+    static_assert(sizeof(Bars) <= 512, "the barriers have 512 bytes");
     volatile int* abort_flag = &bars->abort_flag;
     auto bar = [](const uint64_t& b) { return tc::smem_addr(&b); };
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -115,11 +117,13 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         bars->abort_flag = 0;
         tc::mbar_init(bar(bars->q_full), 1);
         tc::mbar_init(bar(bars->q_free), 1);
-        for (int i = 0; i < NB; ++i) {
+        for (int i = 0; i < ST; ++i) {
             tc::mbar_init(bar(bars->k_full[i]), 1);
             tc::mbar_init(bar(bars->k_empty[i]), 1);
             tc::mbar_init(bar(bars->v_full[i]), 1);
             tc::mbar_init(bar(bars->v_empty[i]), 1);
+        }
+        for (int i = 0; i < NB; ++i) {
             tc::mbar_init(bar(bars->s_full[i]), 1);
             tc::mbar_init(bar(bars->p_full[i]), BM);
         }
@@ -143,65 +147,65 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     const uint32_t tmem = bars->tmem_base;
     const int job_first = ld_global(a.job_start + blockIdx.x), job_last = ld_global(a.job_start + blockIdx.x + 1);
 
-    if (warp == 0) {
-        // ------------------------------------------------------------------ producer (all lanes walk and wait, lane 0 issues)
+    if (warp == 0 || warp == 10) {
+        // ------------------------------------------------------------------ producers: Q and K (warp 0), V (warp 10)
+        // Two warps, because a stage of V is freed long after the stage of K of the same tile: one warp that waits for it would hold up K, whose load then
+        // has one tile's time to arrive (a single row tile of 64 channels 1 250 ns a key tile).  Lane i fetches the i-th box of a tile (pages x 64-channel parts) and
+        // reads its page number a tile ahead.
+        const bool is_v = warp == 10;
         const int page = 1 << a.page_shift, box = min(page, BN);
         const uint32_t box_bytes = (uint32_t)box * 128u, q_bytes = (uint32_t)((BM / a.group) * a.group) * 128u * SUB;
-        uint32_t kv_base[NB] = {};       // key tiles of earlier jobs in every stage
-        uint32_t tails = 0;              // V tiles that got zeros
-        uint32_t k_loads[NB] = {}, v_loads[NB] = {}, q_loads = 0;   // completions that the loads issued so far bring to the barriers
+        const uint32_t ring = is_v ? s_v : s_k;
+        uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
+        const CUtensorMap* map = is_v ? &map_v : &map_k;
+        uint32_t base[ST] = {};          // key tiles of earlier jobs in every stage
+        uint32_t loads[ST] = {}, q_loads = 0, tails = 0;   // completions that the loads issued so far bring to the barriers
         bool ok = true;
         for (int j = job_first; ok && j < job_last; ++j) {
             const CacheJob job = a.jobs[j];
             const CacheSeg seg = a.segs[job.seg + job.pair];   // (of a pair the second row tile sees the most keys)
-            const int token_a = job.pair ? a.segs[job.seg].token0 : seg.token0;
-            if (q_loads > 0 && !(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->q_free), (q_loads - 1) & 1u, abort_flag)))) break;
-            if (lane == 0) {
-                tc::mbar_expect_tx(bar(bars->q_full), job.pair ? 2 * q_bytes : q_bytes);
-                for (int x = 0; x <= job.pair; ++x)
-                    for (int c = 0; c < SUB; ++c)
-                        tma_load_4d(s_q + x * TILE + c * kSubTile, &map_q, bar(bars->q_full), 64 * c, 0, x ? seg.token0 : token_a, job.head);
-            }
-            ++q_loads;
             const int n = job.tile1 - job.tile0;
+            auto page_of = [&](int i) {   // of this lane's box of key tile i
+                const KeyTile t = key_tile(seg, job.tile0 + i);
+                const int p = lane / SUB;
+                return p * box < t.keys ? ld_global(a.table + t.table + (t.key0 >> a.page_shift) + p) : -1;
+            };
+            int32_t id = page_of(0);
+            if (!is_v) {
+                if (q_loads > 0 && !(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->q_free), (q_loads - 1) & 1u, abort_flag)))) break;
+                if (lane == 0) {
+                    tc::mbar_expect_tx(bar(bars->q_full), job.pair ? 2 * q_bytes : q_bytes);
+                    for (int x = 0; x <= job.pair; ++x)
+                        for (int c = 0; c < SUB; ++c)
+                            tma_load_4d(s_q + x * TILE + c * kSubTile, &map_q, bar(bars->q_full), 64 * c, 0, a.segs[job.seg + x].token0, job.head);
+                }
+                ++q_loads;
+            }
 #pragma unroll 1
-            for (int i0 = 0; ok && i0 < n; i0 += NB) {
+            for (int i0 = 0; ok && i0 < n; i0 += ST) {
 #pragma unroll
-                for (int st = 0; st < NB; ++st) {   // key tile i of the job goes to stage i mod NB
+                for (int st = 0; st < ST; ++st) {   // key tile i of the job goes to stage i mod ST
                     const int i = i0 + st;
                     if (!ok || i >= n) break;
-                    const uint32_t fill = kv_base[st] + (uint32_t)(i0 / NB), par = (fill & 1u) ^ 1u;
+                    const uint32_t fill = base[st] + (uint32_t)(i0 / ST);
                     const KeyTile t = key_tile(seg, job.tile0 + i);
-                    const int boxes = (t.keys + box - 1) / box;
-                    const int32_t* pages = a.table + t.table + (t.key0 >> a.page_shift);
-                    const int slot = t.key0 & (page - 1);   // (pages of 256: the second half)
-                    auto load = [&](uint32_t dst, const CUtensorMap* map, uint32_t b) {
-                        for (int p = 0; p < boxes; ++p) {
-                            const int32_t id = ld_global(pages + p);
-                            for (int c = 0; c < SUB; ++c) tma_load_4d(dst + c * kSubTile + p * box_bytes, map, b, 64 * c, slot, job.head, id);
-                        }
-                    };
-                    if (fill > 0 && !(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->k_empty[st]), par, abort_flag)))) break;
-                    if (lane == 0) {
-                        tc::mbar_expect_tx(bar(bars->k_full[st]), boxes * SUB * box_bytes);
-                        load(s_k + st * TILE, &map_k, bar(bars->k_full[st]));
-                    }
-                    k_loads[st] = fill + 1;
-                    if (fill > 0 && !(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->v_empty[st]), par, abort_flag)))) break;
-                    const bool tail = t.keys < BN;
-                    if (lane == 0) {
-                        const uint32_t b = tail ? bar(bars->v_tail) : bar(bars->v_full[st]);
-                        tc::mbar_expect_tx(b, boxes * SUB * box_bytes);
-                        load(s_v + st * TILE, &map_v, b);
-                    }
+                    const int boxes = (t.keys + box - 1) / box, slot = t.key0 & (page - 1);   // (pages of 256: one of two halves)
+                    const bool tail = is_v && t.keys < BN;
+                    const uint32_t b = tail ? bar(bars->v_tail) : bar(full[st]);
+                    if (fill > 0 && !(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(empty[st]), (fill & 1u) ^ 1u, abort_flag)))) break;
+                    if (lane == 0) tc::mbar_expect_tx(b, boxes * SUB * box_bytes);
+                    __syncwarp();
+                    if (lane < boxes * SUB)
+                        tma_load_4d(ring + st * TILE + (lane % SUB) * kSubTile + (lane / SUB) * box_bytes, map, b, 64 * (lane % SUB), slot, job.head, id);
+                    if (i + 1 < n) id = page_of(i + 1);
                     if (!tail) {
-                        v_loads[st] = fill + 1;
+                        loads[st] = fill + 1;
                         continue;
                     }
-                    __syncwarp();
                     ++tails;
+                    __syncwarp();
                     if (!(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->v_tail), (tails - 1) & 1u, abort_flag)))) break;
-                    unsigned char* rows = smem + (2 + NB + st) * TILE;
+                    unsigned char* rows = smem + (2 + ST + st) * TILE;
                     for (int c = 0; c < SUB; ++c)
                         for (int at = t.keys * 8 + lane; at < BN * 8; at += 32) *reinterpret_cast<uint4*>(rows + c * kSubTile + at * 16) = make_uint4(0u, 0u, 0u, 0u);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -210,7 +214,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 }
             }
 #pragma unroll
-            for (int st = 0; st < NB; ++st) kv_base[st] += uses<NB>(n, st);
+            for (int st = 0; st < ST; ++st) base[st] += uses<ST>(n, st);
         }
         if (!ok) {   // somebody gave up: what is still on its way has to land before the CTA leaves
             if (lane == 0) {
@@ -221,10 +225,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 landed(bars->q_full, q_loads);
                 landed(bars->v_tail, tails);
 #pragma unroll
-                for (int st = 0; st < NB; ++st) {
-                    landed(bars->k_full[st], k_loads[st]);
-                    landed(bars->v_full[st], v_loads[st]);
-                }
+                for (int st = 0; st < ST; ++st) landed(full[st], loads[st]);
             }
             __syncwarp();
         }
@@ -255,47 +256,54 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 #pragma unroll
                     for (int k = 0; k < 8; ++k) tc::mma_ts_c<true>(t_o + 64 * c, t_p + 8 * k, dv + c * kSubStep + (uint64_t)(k * 128), idesc_pv);
             };
-            uint32_t kv_base[NB] = {}, sp_base[NB] = {};   // completions before this job: ring stages, score buffers
-            // score tile k = k0 + C of a pair, k0 a multiple of 2 NB (round: parity of k0 / (2 NB))
-            auto step_pair = [&](auto c_c, int k0, uint32_t round, int n_score) -> bool {
-                constexpr int C = decltype(c_c)::value;
-                constexpr int B = C % NB, X = C % 2, ST = (C >> 1) % NB;
-                constexpr int XN = (C + NB) % 2, JN = (C + NB) >> 1, STN = JN % NB;   // score tile k + NB: the next in this buffer
+            // The steps below are unrolled over 2 NB score tiles, so that every operand is a base plus a compile-time offset (operands that are recomputed
+            // per instruction make the issue cost more than the product).  Score tile k of a pair is key tile k / 2 of row tile k mod 2, of a single key
+            // tile k; key tile t of the job lies in stage t mod ST.  With ST = 2 NB a pair's rounds alternate between the halves of the ring (`half`).
+            uint32_t kv_base[ST] = {}, sp_base[NB] = {};   // completions before this job: ring stages, score buffers
+            auto k_full = [&](int st, uint32_t n) { return tc::mbar_wait(bar(bars->k_full[st]), n & 1u, abort_flag); };
+            auto v_full = [&](int st, uint32_t n) { return tc::mbar_wait(bar(bars->v_full[st]), n & 1u, abort_flag); };
+            constexpr int HALVES = ST / NB;
+            // k0: first score tile of the round, r: round.  HALF: its half of the ring
+            auto step_pair = [&](auto c_c, auto half_c, int k0, uint32_t r, int n_score) -> bool {
+                constexpr int C = decltype(c_c)::value, HALF = decltype(half_c)::value;
+                constexpr int B = C % NB, X = C % 2, T0 = HALF * NB + (C >> 1), STAGE = T0 % ST;
+                constexpr int XN = (C + NB) % 2, TN = HALF * NB + ((C + NB) >> 1), STAGEN = TN % ST;   // score tile k + NB: the next in this buffer
                 const uint32_t t_buf = tmem + B * BN, t_o = tmem + NB * BN + X * D;
-                if (X == 0 && !tc::mbar_wait(bar(bars->v_full[ST]), (kv_base[ST] + round) & 1u, abort_flag)) return false;
+                const uint32_t lap = r / HALVES;   // how often the job has been round the ring
+                if (X == 0 && !v_full(STAGE, kv_base[STAGE] + lap)) return false;
                 if (!tc::mbar_wait(bar(bars->p_full[B]), (sp_base[B] + (C / NB)) & 1u, abort_flag)) return false;
                 tc::fence_after_sync();
-                issue_pv(t_o, t_buf + kPColumn, dv0 + ST * kTileStep);
+                issue_pv(t_o, t_buf + kPColumn, dv0 + STAGE * kTileStep);
                 tc::mma_commit(bar(bars->o_done[X]));
-                if (X == 1) tc::mma_commit(bar(bars->v_empty[ST]));
+                if (X == 1) tc::mma_commit(bar(bars->v_empty[STAGE]));
                 if (k0 + C + NB < n_score) {
                     if (XN == 0) {
-                        if (!tc::mbar_wait(bar(bars->k_full[STN]), (kv_base[STN] + round + (JN >= NB ? 1u : 0u)) & 1u, abort_flag)) return false;
+                        if (!k_full(STAGEN, kv_base[STAGEN] + lap + (TN >= ST ? 1u : 0u))) return false;
                         tc::fence_after_sync();
                     }
-                    issue_qk(t_buf, dq0 + XN * kTileStep, dk0 + STN * kTileStep, bar(bars->s_full[B]));
-                    if (XN == 1) tc::mma_commit(bar(bars->k_empty[STN]));
+                    issue_qk(t_buf, dq0 + XN * kTileStep, dk0 + STAGEN * kTileStep, bar(bars->s_full[B]));
+                    if (XN == 1) tc::mma_commit(bar(bars->k_empty[STAGEN]));
                     if (k0 + C + NB + 1 == n_score) tc::mma_commit(bar(bars->q_free));   // that was the job's last S
                 }
                 return true;
             };
-            // score tile k = key tile k = k0 + C of a single row tile, k0 a multiple of 2 NB
-            auto step_single = [&](auto c_c, int k0, int n_single) -> bool {
+            auto step_single = [&](auto c_c, int k0, uint32_t r, int n_single) -> bool {
                 constexpr int C = decltype(c_c)::value;
-                constexpr int B = C % NB, X = C % 2;
-                constexpr uint32_t IDX = C / NB;
+                constexpr int B = C % NB, X = C % 2, STAGE = C % ST, STAGEN = (C + NB) % ST;
                 const uint32_t t_buf = tmem + B * BN, t_o = tmem + NB * BN + X * D;
-                if (!tc::mbar_wait(bar(bars->v_full[B]), (kv_base[B] + IDX) & 1u, abort_flag)) return false;
-                if (!tc::mbar_wait(bar(bars->p_full[B]), (sp_base[B] + IDX) & 1u, abort_flag)) return false;
+                // a round is 2 NB key tiles: once round the ring, or twice
+                const uint32_t lap = r * (2 / HALVES) + C / ST, lap_n = r * (2 / HALVES) + (C + NB) / ST;
+                if (!v_full(STAGE, kv_base[STAGE] + lap)) return false;
+                if (!tc::mbar_wait(bar(bars->p_full[B]), (sp_base[B] + C / NB) & 1u, abort_flag)) return false;
                 tc::fence_after_sync();
-                issue_pv(t_o, t_buf + kPColumn, dv0 + B * kTileStep);
+                issue_pv(t_o, t_buf + kPColumn, dv0 + STAGE * kTileStep);
                 tc::mma_commit(bar(bars->o_done[X]));
-                tc::mma_commit(bar(bars->v_empty[B]));
+                tc::mma_commit(bar(bars->v_empty[STAGE]));
                 if (k0 + C + NB < n_single) {
-                    if (!tc::mbar_wait(bar(bars->k_full[B]), (kv_base[B] + IDX + 1u) & 1u, abort_flag)) return false;
+                    if (!k_full(STAGEN, kv_base[STAGEN] + lap_n)) return false;
                     tc::fence_after_sync();
-                    issue_qk(t_buf, dq0, dk0 + B * kTileStep, bar(bars->s_full[B]));
-                    tc::mma_commit(bar(bars->k_empty[B]));
+                    issue_qk(t_buf, dq0, dk0 + STAGEN * kTileStep, bar(bars->s_full[B]));
+                    tc::mma_commit(bar(bars->k_empty[STAGEN]));
                     if (k0 + C + NB + 1 == n_single) tc::mma_commit(bar(bars->q_free));
                 }
                 return true;
@@ -313,7 +321,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     if (k >= n_score) break;
                     const int tile = job.pair ? k >> 1 : k, x = job.pair ? k & 1 : 0;
                     if (x == 0) {
-                        if (!(ok = tc::mbar_wait(bar(bars->k_full[tile]), kv_base[tile] & 1u, abort_flag))) break;
+                        if (!(ok = k_full(tile, kv_base[tile]))) break;
                         tc::fence_after_sync();
                     }
                     issue_qk(tmem + k * BN, dq0 + x * kTileStep, dk0 + tile * kTileStep, bar(bars->s_full[k]));
@@ -321,37 +329,50 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     if (k + 1 == n_score) tc::mma_commit(bar(bars->q_free));
                 }
                 if (!ok) break;
-                uint32_t round = 0;
-                for (int k0 = 0; ok && k0 < n_score; k0 += 2 * NB, round ^= 1u) {
-                    auto run = [&](auto c_c) {
-                        if (ok && k0 + decltype(c_c)::value < n_score)
-                            ok = job.pair ? step_pair(c_c, k0, round, n_score) : step_single(c_c, k0, n_score);
-                    };
-                    run(std::integral_constant<int, 0>{});
-                    run(std::integral_constant<int, 1>{});
-                    run(std::integral_constant<int, 2>{});
-                    run(std::integral_constant<int, 3>{});
+                uint32_t r = 0;
+                auto all = [&](auto step) {   // one round
+                    step(std::integral_constant<int, 0>{});
+                    step(std::integral_constant<int, 1>{});
+                    step(std::integral_constant<int, 2>{});
+                    step(std::integral_constant<int, 3>{});
                     if constexpr (NB == 3) {
-                        run(std::integral_constant<int, 4>{});
-                        run(std::integral_constant<int, 5>{});
+                        step(std::integral_constant<int, 4>{});
+                        step(std::integral_constant<int, 5>{});
                     }
+                };
+                if (job.pair) {
+                    for (int k0 = 0; ok && k0 < n_score; k0 += 2 * NB, ++r) {
+                        all([&](auto c) {
+                            if (ok && k0 + decltype(c)::value < n_score) ok = step_pair(c, std::integral_constant<int, 0>{}, k0, r, n_score);
+                        });
+                        if constexpr (HALVES == 2) {
+                            k0 += 2 * NB, ++r;
+                            all([&](auto c) {
+                                if (ok && k0 + decltype(c)::value < n_score) ok = step_pair(c, std::integral_constant<int, 1>{}, k0, r, n_score);
+                            });
+                        }
+                    }
+                } else {
+                    for (int k0 = 0; ok && k0 < n_score; k0 += 2 * NB, ++r)
+                        all([&](auto c) {
+                            if (ok && k0 + decltype(c)::value < n_score) ok = step_single(c, k0, r, n_score);
+                        });
                 }
                 if (ok) tc::mma_commit(bar(bars->o_final));
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    sp_base[b] += uses<NB>(n_score, b);
-                    kv_base[b] += uses<NB>(n, b);
-                }
+                for (int b = 0; b < NB; ++b) sp_base[b] += uses<NB>(n_score, b);
+#pragma unroll
+                for (int st = 0; st < ST; ++st) kv_base[st] += uses<ST>(n, st);
             }
         }
         __syncwarp();
-    } else {
+    } else {   // warps 2 .. 9
         // ------------------------------------------------------------------ softmax and results
         const int x = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;   // group; row of the tile = lane of tensor memory
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_o = tmem + NB * BN + x * D + lane_addr;
         uint32_t sp_base[NB] = {}, od_base = 0, singles = 0;
-        float2* xch = reinterpret_cast<float2*>(smem + (2 + 2 * NB) * TILE + 512);
+        float2* xch = reinterpret_cast<float2*>(smem + (2 + 2 * ST) * TILE + 512);
         bool ok = true;
         int jobs = 0;
         for (int jb = job_first; ok && jb < job_last; ++jb, ++jobs) {
