@@ -60,7 +60,7 @@ struct RowsGradTensor {
     int64_t x_head, x_token, dy_head, dy_token, dx_head, dx_token;
     const float* weight;
     float *dweight, *dbias;   // [head_dim] or null
-    int32_t heads, chunks;
+    int32_t heads, chunks, ctas;
 };
 struct RowsGradArgs {
     RowsGradTensor t[2];
@@ -69,13 +69,14 @@ struct RowsGradArgs {
     int64_t n_tokens;
     float eps;
     int32_t norm;
-    float* partial;     // [tensor][CTA][2][head_dim]
+    float* partial;     // [CTA of q, then of k][2][head_dim]
     int32_t* arrived;   // [tensor], zero between launches
     int32_t* status;
 };
 cudaError_t launch_rows(const RowsArgs& a, int head_dim, int dtype, int sm_count, cudaStream_t stream);
 cudaError_t launch_rows_grad(const RowsGradArgs& a, int head_dim, int dtype, int sm_count, cudaStream_t stream);
-size_t rows_grad_partial_floats(int head_dim, int sm_count);
+size_t rows_grad_partial_floats(int head_dim, int chunks, int sm_count);
+int rows_grad_chunks(int heads);
 
 // What httm_cache_append needs of a rotary handle.
 struct RotaryView {

@@ -21,13 +21,14 @@
 #include "httm_cache.h"
 #include "httm_internal.h"
 #include "httm_launch.cuh"
+#include "tc_sm100.cuh"
 
 namespace httm {
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kHeadsPerChunk = 4;       // rows a lane has in flight
+constexpr int kHeadsPerChunk = 4;       // rows that a lane takes of a token
 constexpr int kGradHeadsPerChunk = 2;   // (two tensors are read)
 
 template <typename T>
@@ -49,23 +50,48 @@ struct Pair2<__half> {
     }
 };
 
-__device__ __forceinline__ uint2 ld_row(const void* p) {   // behind depend_wait, and the row is read once
-    uint2 v;
-    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-    return v;
+// A warp's rows on their way in: a ring of kStages stages, each with kRowsAtOnce rows per group of lanes (512 bytes a warp).  Lane l of a row copies its
+// 16-byte piece l and reads the two 8-byte pieces it computes with; pieces of odd rows lie exchanged, so that two rows' reads meet in no bank.
+constexpr int kStages = 2, kRowsAtOnce = 4;
+constexpr int kRingBytes = kStages * kRowsAtOnce * 512;   // of a warp
+template <int LANES>
+struct Ring {
+    uint32_t at;      // this lane's row in stage 0
+    uint32_t piece;   // where its piece goes in there
+    int flip;
+    __device__ __forceinline__ Ring(unsigned char* smem, int lane) {
+        const int row = (threadIdx.x & 31) / LANES;
+        flip = (row & 1 ? 6 : 0) & (LANES - 1);
+        at = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + (threadIdx.x >> 5) * kRingBytes + row * (LANES * 16);
+        piece = (uint32_t)((lane ^ flip) << 4);
+    }
+    __device__ __forceinline__ void copy(int stage, int i, const void* row, bool valid) const {
+        if (valid)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + (uint32_t)((stage * kRowsAtOnce + i) * 512) + piece), "l"(row) : "memory");
+    }
+    __device__ __forceinline__ uint2 read(int stage, int i, int channel) const {   // four channels
+        uint2 v;
+        const uint32_t from = at + (uint32_t)((stage * kRowsAtOnce + i) * 512) + (uint32_t)((((channel >> 3) ^ flip) << 4) | ((channel & 4) << 1));
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(from) : "memory");
+        return v;
+    }
+    static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    static __device__ __forceinline__ void arrived() {   // the oldest stage is there for the whole warp, and the one before it has been read
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+        __syncwarp();
+    }
+};
+template <typename T>
+__device__ __forceinline__ void unpack4(uint2 w, float2* v) {
+    v[0] = Pair2<T>::load(w.x), v[1] = Pair2<T>::load(w.y);
 }
 template <typename T>
-__device__ __forceinline__ void unpack4(uint2 w, float* v) {
-    const float2 a = Pair2<T>::load(w.x), b = Pair2<T>::load(w.y);
-    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
-}
-template <typename T>
-__device__ __forceinline__ uint2 pack4(const float* v) {
-    return make_uint2(Pair2<T>::store(v[0], v[1]), Pair2<T>::store(v[2], v[3]));
+__device__ __forceinline__ uint2 pack4(const float2* v) {
+    return make_uint2(Pair2<T>::store(v[0].x, v[0].y), Pair2<T>::store(v[1].x, v[1].y));
 }
 
-// The channels of lane `l` of a row: v[0..3] are channels a .. a + 3, v[4..7] channels b .. b + 3.  Halves: pair i is (v[i], v[4 + i]); interleaved: the
-// pairs are (v[0], v[1]), (v[2], v[3]), (v[4], v[5]), (v[6], v[7]).
+// The channels of lane `l` of a row: v[0], v[1] are channels a .. a + 3, v[2], v[3] channels b .. b + 3, two to a register pair (one instruction does both).
+// Halves: pair i of the lane is channel i of the first four and of the last four; interleaved: each register pair is a pair.
 struct LaneChannels {
     int a, b, axis, first;   // first of the four frequencies
     bool rotates;
@@ -85,36 +111,41 @@ struct LaneChannels {
     }
 };
 struct Turn {   // cos and sin of the lane's four pairs
-    float c[4], s[4];
+    float2 c[2], s[2];
 };
-__device__ __forceinline__ Turn load_turn(const RotationTable& t, const LaneChannels& ch, const int32_t* positions, int64_t token, int32_t* status) {
-    Turn r;
-    const int32_t p = ld_global(positions + token * t.axes + ch.axis);
-    if ((uint32_t)p >= (uint32_t)t.n_positions) {   // no such row of the table
+__device__ __forceinline__ Turn load_turn(const RotationTable& t, const LaneChannels& ch, int32_t position, int32_t* status) {
+    float4 u, v;
+    if ((uint32_t)position < (uint32_t)t.n_positions) {
+        const float4* at = reinterpret_cast<const float4*>(t.cos_sin + (int64_t)position * t.half + ch.first);
+        u = __ldg(at), v = __ldg(at + 1);
+    } else {   // no such row of the table
         atomicCAS(status, kDevOk, kDevBadIndex);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.c[i] = r.s[i] = __int_as_float(0x7fc00000);
-        return r;
+        u.x = u.y = u.z = u.w = __int_as_float(0x7fc00000);
+        v = u;
     }
-    const float4* at = reinterpret_cast<const float4*>(t.cos_sin + (int64_t)p * t.half + ch.first);
-    const float4 u = __ldg(at), v = __ldg(at + 1);
-    r.c[0] = u.x, r.s[0] = u.y, r.c[1] = u.z, r.s[1] = u.w;
-    r.c[2] = v.x, r.s[2] = v.y, r.c[3] = v.z, r.s[3] = v.w;
+    Turn r;
+    r.c[0] = make_float2(u.x, u.z), r.c[1] = make_float2(v.x, v.z);
+    r.s[0] = make_float2(u.y, u.w), r.s[1] = make_float2(v.y, v.w);
     return r;
 }
+// BACK: by the opposite angles
 template <bool BACK>
-__device__ __forceinline__ void turn(float (&v)[8], const Turn& t, bool interleaved) {
-    auto one = [](float& a, float& b, float c, float s) {
-        const float u = BACK ? fmaf(a, c, b * s) : fmaf(a, c, -(b * s));
-        b = BACK ? fmaf(b, c, -(a * s)) : fmaf(a, s, b * c);
-        a = u;
-    };
+__device__ __forceinline__ void turn(float2 (&v)[4], const Turn& t, bool interleaved) {
     if (interleaved) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) one(v[2 * i], v[2 * i + 1], t.c[i], t.s[i]);
+        for (int i = 0; i < 4; ++i) {
+            const float c = i & 1 ? t.c[i >> 1].y : t.c[i >> 1].x, s = (BACK ? -1.f : 1.f) * (i & 1 ? t.s[i >> 1].y : t.s[i >> 1].x), x = v[i].x;
+            v[i].x = fmaf(x, c, -(v[i].y * s));
+            v[i].y = fmaf(v[i].y, c, x * s);
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) one(v[i], v[4 + i], t.c[i], t.s[i]);
+        for (int i = 0; i < 2; ++i) {
+            const float2 a = v[i], b = v[2 + i], as = tc::fmul2(a, t.s[i]), bs = tc::fmul2(b, t.s[i]);
+            const float2 ac = tc::fmul2(a, t.c[i]), bc = tc::fmul2(b, t.c[i]);
+            v[i] = BACK ? tc::fadd2(ac, bs) : tc::fsub2(ac, bs);
+            v[2 + i] = BACK ? tc::fsub2(bc, as) : tc::fadd2(bc, as);
+        }
     }
 }
 template <int LANES>
@@ -123,37 +154,40 @@ __device__ __forceinline__ float row_sum(float v) {
     for (int o = 1; o < LANES; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+__device__ __forceinline__ float sum8(const float2 (&x)[4]) {
+    const float2 s = tc::fadd2(tc::fadd2(x[0], x[1]), tc::fadd2(x[2], x[3]));
+    return s.x + s.y;
+}
 // x -> xh in place; returns r.  The mean is taken off before the squares are added up: a row far from zero keeps its digits.
 template <int LANES>
-__device__ __forceinline__ float normalise(float (&x)[8], int norm, float eps) {
+__device__ __forceinline__ float normalise(float2 (&x)[4], int norm, float eps) {
     constexpr float kInv = 1.0f / (8 * LANES);
     if (norm == HTTM_NORM_LAYER) {
-        const float mean = row_sum<LANES>(((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]))) * kInv;
+        const float mean = row_sum<LANES>(sum8(x)) * -kInv;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] -= mean;
+        for (int i = 0; i < 4; ++i) x[i] = tc::fadd2(x[i], make_float2(mean, mean));
     }
-    float q0 = x[0] * x[0], q1 = x[1] * x[1];
+    const float2 q = tc::ffma2(x[3], x[3], tc::ffma2(x[2], x[2], tc::ffma2(x[1], x[1], tc::fmul2(x[0], x[0]))));
+    const float r = rsqrtf(fmaf(row_sum<LANES>(q.x + q.y), kInv, eps));
 #pragma unroll
-    for (int i = 2; i < 8; i += 2) q0 = fmaf(x[i], x[i], q0), q1 = fmaf(x[i + 1], x[i + 1], q1);
-    const float r = rsqrtf(fmaf(row_sum<LANES>(q0 + q1), kInv, eps));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= r;
+    for (int i = 0; i < 4; ++i) x[i] = tc::fmul2(x[i], make_float2(r, r));
     return r;
 }
-__device__ __forceinline__ void load_channels(const float* p, const LaneChannels& ch, float (&v)[8], float without) {
+__device__ __forceinline__ void load_channels(const float* p, const LaneChannels& ch, float2 (&v)[4], float without) {
     if (p) {
-        const float4 a = make_float4(p[ch.a], p[ch.a + 1], p[ch.a + 2], p[ch.a + 3]);
-        const float4 b = make_float4(p[ch.b], p[ch.b + 1], p[ch.b + 2], p[ch.b + 3]);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        v[0] = make_float2(p[ch.a], p[ch.a + 1]), v[1] = make_float2(p[ch.a + 2], p[ch.a + 3]);
+        v[2] = make_float2(p[ch.b], p[ch.b + 1]), v[3] = make_float2(p[ch.b + 2], p[ch.b + 3]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = without;
+        for (int i = 0; i < 4; ++i) v[i] = make_float2(without, without);
     }
 }
 
 template <typename T, int LANES, bool PAGED>
-__global__ void __launch_bounds__(kThreads) rows_kernel(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) rows_kernel(const __grid_constant__ RowsArgs a) {
     constexpr int GROUPS = kThreads / LANES;
+    static_assert(kHeadsPerChunk == kRowsAtOnce, "a stage holds a chunk of heads");
+    __shared__ __align__(128) unsigned char smem[kThreads / 32 * kRingBytes];
     const bool second = (int)blockIdx.y >= a.t[0].chunks;
     const RowsTensor& t = a.t[second ? 1 : 0];
     const int h0 = ((int)blockIdx.y - (second ? a.t[0].chunks : 0)) * kHeadsPerChunk;
@@ -161,139 +195,160 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(const __grid_constant__ 
     RotationTable table = a.table;
     if (!t.rotate) table.rotated_dim = 0;
     const LaneChannels ch(table, lane);
+    const Ring<LANES> ring(smem, lane);
     const int rows = min(kHeadsPerChunk, t.heads - h0);
     depend_wait();
     dependents_launch();
-    float w[8], b[8];
+    const T* in = static_cast<const T*>(t.in) + h0 * t.in_head + 8 * lane;
+    T* out = static_cast<T*>(t.out) + h0 * t.out_head;
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t token = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
+    auto fetch = [&](int stage, int64_t of) {
+#pragma unroll
+        for (int i = 0; i < kHeadsPerChunk; ++i) ring.copy(stage, i, in + of * t.in_token + i * t.in_head, of < a.n_tokens && i < rows);
+        ring.commit();
+    };
+    for (int i = 0; i < kStages - 1; ++i) fetch(i, token + i * step);
+    float2 w[4], b[4];
     load_channels(t.weight, ch, w, 1.f);
     load_channels(t.bias, ch, b, -0.f);   // (x + -0 is x, a zero's sign included)
-    const T* in = static_cast<const T*>(t.in) + h0 * t.in_head;
-    T* out = static_cast<T*>(t.out) + h0 * t.out_head;
+    // a token's position and place are read one turn ahead: the table's row is not another trip to memory behind them
+    int32_t position = 0, slot = 0;
+    auto look_ahead = [&](int64_t next) {
+        if (next >= a.n_tokens) return;
+        if (ch.rotates) position = ld_global(a.positions + next * table.axes + ch.axis);
+        if (PAGED) slot = ld_global(a.slots + next);
+    };
+    look_ahead(token);
     // (all lanes of a warp go through the loop together: the sums over a row exchange between lanes)
-    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < a.n_tokens; first += (int64_t)gridDim.x * GROUPS) {
-        const int64_t token = first + threadIdx.x / LANES;
+    int stage = 0;
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < a.n_tokens; first += step, token += step) {
         const bool here = token < a.n_tokens;
-        uint2 raw[kHeadsPerChunk][2];
-        const T* src = in + token * t.in_token;
-#pragma unroll
-        for (int i = 0; i < kHeadsPerChunk; ++i) {
-            if (here && i < rows) {
-                raw[i][0] = ld_row(src + i * t.in_head + ch.a);
-                raw[i][1] = ld_row(src + i * t.in_head + ch.b);
-            } else {
-                raw[i][0] = raw[i][1] = make_uint2(0u, 0u);
-            }
-        }
         Turn cs;
-        if (here && ch.rotates) cs = load_turn(table, ch, a.positions, token, a.status);
+        if (here && ch.rotates) cs = load_turn(table, ch, position, a.status);
         T* dst = out;
-        if (here) {
-            if (PAGED) {
-                const int32_t slot = ld_global(a.slots + token);
-                dst += (int64_t)(slot >> a.page_shift) * t.out_page + (int64_t)(slot & ((1 << a.page_shift) - 1)) * t.out_token;
-            } else {
-                dst += token * t.out_token;
-            }
-        }
+        if (PAGED)
+            dst += (int64_t)(slot >> a.page_shift) * t.out_page + (int64_t)(slot & ((1 << a.page_shift) - 1)) * t.out_token;
+        else
+            dst += token * t.out_token;
+        look_ahead(token + step);
+        ring.arrived();
+        fetch(stage == 0 ? kStages - 1 : stage - 1, token + (kStages - 1) * step);
 #pragma unroll
         for (int i = 0; i < kHeadsPerChunk; ++i) {
-            float x[8];
-            unpack4<T>(raw[i][0], x);
-            unpack4<T>(raw[i][1], x + 4);
-            if (t.norm != HTTM_NORM_NONE) {
-                normalise<LANES>(x, t.norm, a.eps);
-            }
+            float2 x[4];   // (a row that does not exist: whatever the stage holds, not stored)
+            unpack4<T>(ring.read(stage, i, ch.a), x);
+            unpack4<T>(ring.read(stage, i, ch.b), x + 2);
+            if (t.norm != HTTM_NORM_NONE) normalise<LANES>(x, t.norm, a.eps);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) x[c] = fmaf(x[c], w[c], b[c]);
+            for (int c = 0; c < 4; ++c) x[c] = tc::ffma2(x[c], w[c], b[c]);
             if (ch.rotates) turn<false>(x, cs, table.interleaved != 0);
             if (here && i < rows) {
                 *reinterpret_cast<uint2*>(dst + i * t.out_head + ch.a) = pack4<T>(x);
-                *reinterpret_cast<uint2*>(dst + i * t.out_head + ch.b) = pack4<T>(x + 4);
+                *reinterpret_cast<uint2*>(dst + i * t.out_head + ch.b) = pack4<T>(x + 2);
             }
         }
+        stage = stage == kStages - 1 ? 0 : stage + 1;
     }
 }
 
-// Gradients.  A CTA keeps to one tensor; its threads add up what they see of dw and db in registers, the CTA adds those up in shared memory, and the
-// CTA of a tensor that arrives last adds the CTAs' sums, in the order of their numbers: the same sizes give the same bits.
+// Gradients.  A CTA keeps to one tensor and one chunk of its heads; its threads add up what they see of dw and db in registers, the CTA adds those up in
+// shared memory, and the CTA of a tensor that arrives last adds the CTAs' sums, in the order of their numbers: the same sizes give the same bits.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(kThreads) rows_grad_kernel(const __grid_constant__ RowsGradArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) rows_grad_kernel(const __grid_constant__ RowsGradArgs a) {
     constexpr int GROUPS = kThreads / LANES, D = 8 * LANES;
-    __shared__ float sums[2][GROUPS][D];
-    __shared__ bool last;
-    const int which = blockIdx.y;
+    static_assert(2 * kGradHeadsPerChunk == kRowsAtOnce, "a stage holds a chunk of heads of both tensors");
+    __shared__ __align__(128) unsigned char smem[kThreads / 32 * kRingBytes];
+    const int which = (int)blockIdx.x >= a.t[0].ctas ? 1 : 0;
     const RowsGradTensor& t = a.t[which];
+    const int cta = (int)blockIdx.x - (which ? a.t[0].ctas : 0), chunk = cta % t.chunks, column = cta / t.chunks;
+    const int h0 = chunk * kGradHeadsPerChunk, rows = min(kGradHeadsPerChunk, t.heads - h0);
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     const LaneChannels ch(a.table, lane);
+    const Ring<LANES> ring(smem, lane);
     depend_wait();
     dependents_launch();
-    float w[8], dw[8], db[8];
+    const T *xs = static_cast<const T*>(t.x) + h0 * t.x_head + 8 * lane, *dys = static_cast<const T*>(t.dy) + h0 * t.dy_head + 8 * lane;
+    T* dxs = static_cast<T*>(t.dx) + h0 * t.dx_head;
+    const int64_t step = (int64_t)(t.ctas / t.chunks) * GROUPS;
+    int64_t token = (int64_t)column * GROUPS + group;
+    auto fetch = [&](int stage, int64_t of) {
+#pragma unroll
+        for (int i = 0; i < kGradHeadsPerChunk; ++i) {
+            const bool valid = of < a.n_tokens && i < rows;
+            ring.copy(stage, 2 * i, xs + of * t.x_token + i * t.x_head, valid);
+            ring.copy(stage, 2 * i + 1, dys + of * t.dy_token + i * t.dy_head, valid);
+        }
+        ring.commit();
+    };
+    for (int i = 0; i < kStages - 1; ++i) fetch(i, token + i * step);
+    float2 w[4], dw[4], db[4];
     load_channels(t.weight, ch, w, 1.f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dw[i] = db[i] = 0.f;
-    const T *xs = static_cast<const T*>(t.x), *dys = static_cast<const T*>(t.dy);
-    T* dxs = static_cast<T*>(t.dx);
-    const int64_t units = a.n_tokens * t.chunks;   // (token, chunk of heads)
-    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < units; first += (int64_t)gridDim.x * GROUPS) {
-        const int64_t unit = first + group;
-        const bool here = unit < units;
-        const int64_t token = here ? unit / t.chunks : 0;
-        const int h0 = here ? (int)(unit - token * t.chunks) * kGradHeadsPerChunk : 0;
-        const int rows = here ? min(kGradHeadsPerChunk, t.heads - h0) : 0;
-        uint2 rx[kGradHeadsPerChunk][2], rg[kGradHeadsPerChunk][2];
-#pragma unroll
-        for (int i = 0; i < kGradHeadsPerChunk; ++i) {
-            const T* x = xs + (h0 + i) * t.x_head + token * t.x_token;
-            const T* dy = dys + (h0 + i) * t.dy_head + token * t.dy_token;
-            if (i < rows) {
-                rx[i][0] = ld_row(x + ch.a), rx[i][1] = ld_row(x + ch.b);
-                rg[i][0] = ld_row(dy + ch.a), rg[i][1] = ld_row(dy + ch.b);
-            } else {
-                rx[i][0] = rx[i][1] = rg[i][0] = rg[i][1] = make_uint2(0u, 0u);
-            }
-        }
+    for (int i = 0; i < 4; ++i) dw[i] = db[i] = make_float2(0.f, 0.f);
+    int32_t position = 0;
+    if (token < a.n_tokens && ch.rotates) position = ld_global(a.positions + token * a.table.axes + ch.axis);
+    int stage = 0;
+    for (int64_t first = (int64_t)column * GROUPS; first < a.n_tokens; first += step, token += step) {
+        const bool here = token < a.n_tokens;
         Turn cs;
-        if (here && ch.rotates) cs = load_turn(a.table, ch, a.positions, token, a.status);
+        if (here && ch.rotates) cs = load_turn(a.table, ch, position, a.status);
+        if (token + step < a.n_tokens && ch.rotates) position = ld_global(a.positions + (token + step) * a.table.axes + ch.axis);
+        ring.arrived();
+        fetch(stage == 0 ? kStages - 1 : stage - 1, token + (kStages - 1) * step);
 #pragma unroll
         for (int i = 0; i < kGradHeadsPerChunk; ++i) {
-            float x[8], g[8];
-            unpack4<T>(rx[i][0], x);
-            unpack4<T>(rx[i][1], x + 4);
-            unpack4<T>(rg[i][0], g);
-            unpack4<T>(rg[i][1], g + 4);
-            if (ch.rotates) turn<true>(g, cs, a.table.interleaved != 0);
+            const bool exists = here && i < rows;
+            float2 x[4], g[4];
+            unpack4<T>(ring.read(stage, 2 * i, ch.a), x);
+            unpack4<T>(ring.read(stage, 2 * i, ch.b), x + 2);
+            unpack4<T>(ring.read(stage, 2 * i + 1, ch.a), g);
+            unpack4<T>(ring.read(stage, 2 * i + 1, ch.b), g + 2);
+            if (ch.rotates && here) turn<true>(g, cs, a.table.interleaved != 0);
             float r = 1.f;
             if (a.norm != HTTM_NORM_NONE) r = normalise<LANES>(x, a.norm, a.eps);
-            if (i < rows) {
+            if (exists) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) dw[c] = fmaf(g[c], x[c], dw[c]), db[c] += g[c];
+                for (int c = 0; c < 4; ++c) dw[c] = tc::ffma2(g[c], x[c], dw[c]), db[c] = tc::fadd2(db[c], g[c]);
             }
 #pragma unroll
-            for (int c = 0; c < 8; ++c) g[c] *= w[c];
+            for (int c = 0; c < 4; ++c) g[c] = tc::fmul2(g[c], w[c]);
             if (a.norm != HTTM_NORM_NONE) {
-                float su = 0.f, sux = 0.f;
+                const float2 ux = tc::ffma2(g[3], x[3], tc::ffma2(g[2], x[2], tc::ffma2(g[1], x[1], tc::fmul2(g[0], x[0]))));
+                const float mux = row_sum<LANES>(ux.x + ux.y) * (-1.0f / D);
+                if (a.norm == HTTM_NORM_LAYER) {
+                    const float mu = row_sum<LANES>(sum8(g)) * (-1.0f / D);
 #pragma unroll
-                for (int c = 0; c < 8; ++c) su += g[c], sux = fmaf(g[c], x[c], sux);
-                sux = row_sum<LANES>(sux) * (1.0f / D);
-                su = a.norm == HTTM_NORM_LAYER ? row_sum<LANES>(su) * (1.0f / D) : 0.f;
+                    for (int c = 0; c < 4; ++c) g[c] = tc::fadd2(g[c], make_float2(mu, mu));
+                }
 #pragma unroll
-                for (int c = 0; c < 8; ++c) g[c] = r * (g[c] - su - x[c] * sux);
+                for (int c = 0; c < 4; ++c) g[c] = tc::fmul2(make_float2(r, r), tc::ffma2(x[c], make_float2(mux, mux), g[c]));
             }
-            if (i < rows) {
-                T* dx = dxs + (h0 + i) * t.dx_head + token * t.dx_token;
+            if (exists) {
+                T* dx = dxs + i * t.dx_head + token * t.dx_token;
                 *reinterpret_cast<uint2*>(dx + ch.a) = pack4<T>(g);
-                *reinterpret_cast<uint2*>(dx + ch.b) = pack4<T>(g + 4);
+                *reinterpret_cast<uint2*>(dx + ch.b) = pack4<T>(g + 2);
             }
         }
+        stage = stage == kStages - 1 ? 0 : stage + 1;
     }
     if (!t.dweight && !t.dbias) return;
+    __syncthreads();   // (no copies are in flight behind the last token: the ring's memory is free)
+    auto sums = reinterpret_cast<float(*)[GROUPS][D]>(smem);   // [2]
+    static_assert(2 * GROUPS * D * 4 <= sizeof(smem), "the sums have their place");
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        sums[0][group][ch.a + c] = dw[c], sums[0][group][ch.b + c] = dw[4 + c];
-        sums[1][group][ch.a + c] = db[c], sums[1][group][ch.b + c] = db[4 + c];
+    for (int c = 0; c < 2; ++c) {
+        const int at[2] = {ch.a + 2 * c, ch.b + 2 * c};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            *reinterpret_cast<float2*>(&sums[0][group][at[k]]) = dw[2 * k + c];
+            *reinterpret_cast<float2*>(&sums[1][group][at[k]]) = db[2 * k + c];
+        }
     }
     __syncthreads();
-    float* mine = a.partial + ((int64_t)which * gridDim.x + blockIdx.x) * 2 * D;
+    // partial sums of all CTAs of q, then of k
+    float* all = a.partial + (which ? (int64_t)a.t[0].ctas * 2 * D : 0);
+    float* mine = all + (int64_t)cta * 2 * D;
     for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
         float v = 0.f;
 #pragma unroll 8
@@ -302,28 +357,28 @@ __global__ void __launch_bounds__(kThreads) rows_grad_kernel(const __grid_consta
     }
     __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(a.arrived + which, 1) == (int)gridDim.x - 1;
-    __syncthreads();
-    if (!last) return;
+    if (!__syncthreads_or(threadIdx.x == 0 && atomicAdd(a.arrived + which, 1) == t.ctas - 1)) return;
     __threadfence();
-    const float* all = a.partial + (int64_t)which * gridDim.x * 2 * D;
-    // each of `parts` threads per sum takes every parts-th CTA
-    constexpr int PARTS = 2 * D >= kThreads ? 1 : kThreads / (2 * D);
-    float* flat = &sums[0][0][0];
-    for (int i = threadIdx.x; i < 2 * D * PARTS; i += kThreads) {
-        const int at = i % (2 * D);
-        float v = 0.f;
+    // four sums per thread; `PARTS` threads share them, each takes every PARTS-th CTA
+    constexpr int QUADS = 2 * D / 4, PARTS = kThreads / QUADS;
+    const int quad = threadIdx.x % QUADS, part = threadIdx.x / QUADS;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 16
-        for (int c = i / (2 * D); c < (int)gridDim.x; c += PARTS) v += __ldcg(all + (int64_t)c * 2 * D + at);
-        flat[i] = v;
+    for (int c = part; c < t.ctas; c += PARTS) {
+        const float4 u = __ldcg(reinterpret_cast<const float4*>(all + (int64_t)c * 2 * D) + quad);
+        v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
     }
+    float4* flat = reinterpret_cast<float4*>(smem);
+    flat[threadIdx.x] = v;   // (`sums` has been read by all threads)
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
-        float v = 0.f;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) v += flat[p * 2 * D + i];
-        float* to = i < D ? t.dweight : t.dbias;
-        if (to) to[i % D] = v;
+    if (part == 0) {
+        for (int p = 1; p < PARTS; ++p) {
+            const float4 u = flat[p * QUADS + quad];
+            v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+        }
+        float* to = 4 * quad < D ? t.dweight : t.dbias;
+        const int at = 4 * quad % D;
+        if (to) to[at] = v.x, to[at + 1] = v.y, to[at + 2] = v.z, to[at + 3] = v.w;
     }
     if (threadIdx.x == 0) a.arrived[which] = 0;
 }
@@ -356,7 +411,6 @@ cudaError_t launch_rows_grad_of(const RowsGradArgs& a, int head_dim, dim3 grid, 
     }
     return cudaErrorInvalidValue;
 }
-int grad_ctas(int sm_count) { return 2 * sm_count; }   // of each tensor
 
 }  // namespace
 
@@ -365,28 +419,36 @@ cudaError_t launch_rows(const RowsArgs& args, int head_dim, int dtype, int sm_co
     int chunks = 0;
     for (RowsTensor& t : a.t) chunks += t.chunks = (t.heads + kHeadsPerChunk - 1) / kHeadsPerChunk;
     const int groups = kThreads / (head_dim / 8);
-    const int64_t all = (a.n_tokens + groups - 1) / groups, most = ((int64_t)sm_count * 8 + chunks - 1) / chunks;
-    const dim3 grid((unsigned)(all < most ? all : most), (unsigned)chunks);
+    // three CTAs to an SM, all resident at once: one more and the call takes a second round for it (scene of 32 976 tokens: 448 CTAs 66.5 us, 440 48.6)
+    const int64_t all = (a.n_tokens + groups - 1) / groups, most = 3 * sm_count / chunks, x = all < most ? all : most;
+    const dim3 grid((unsigned)(x < 1 ? 1 : x), (unsigned)chunks);
     if (dtype == HTTM_BF16)
         return a.slots ? launch_rows_of<__nv_bfloat16, true>(a, head_dim, grid, stream) : launch_rows_of<__nv_bfloat16, false>(a, head_dim, grid, stream);
     return a.slots ? launch_rows_of<__half, true>(a, head_dim, grid, stream) : launch_rows_of<__half, false>(a, head_dim, grid, stream);
 }
 
-size_t rows_grad_partial_floats(int head_dim, int sm_count) { return (size_t)2 * grad_ctas(sm_count) * 2 * head_dim; }
+// CTAs of the gradients' kernel for one tensor: one to an SM (two tensors: two; scene of 32 976 tokens 95 us, with two each 107), more where a tensor has more
+// rows than that (queries that share key heads would otherwise have half the SM's warps to themselves), at least one for each chunk of heads.  The number
+// depends on the tensor alone, and with it the order of its sums: the gradients of k are the same bits with and without q.
+constexpr int kGradRows = 3600, kMostGradCtas = 8;   // rows of a CTA where there are more of them than SMs; CTAs per SM
+static int64_t grad_ctas(int64_t tokens, int heads, int chunks, int groups, int sm_count) {
+    const int64_t all = (tokens + groups - 1) / groups, by_rows = tokens * heads / kGradRows;
+    const int64_t some = by_rows < sm_count ? sm_count : by_rows < kMostGradCtas * sm_count ? by_rows : kMostGradCtas * sm_count;
+    const int64_t most = some / chunks, x = all < most ? all : most;
+    return (x < 1 ? 1 : x) * chunks;
+}
+size_t rows_grad_partial_floats(int head_dim, int chunks, int sm_count) { return (size_t)(2 * kMostGradCtas * sm_count + chunks) * 2 * head_dim; }
+
+int rows_grad_chunks(int heads) { return (heads + kGradHeadsPerChunk - 1) / kGradHeadsPerChunk; }
 
 cudaError_t launch_rows_grad(const RowsGradArgs& args, int head_dim, int dtype, int sm_count, cudaStream_t stream) {
     RowsGradArgs a = args;
-    int64_t units = 1;
-    int tensors = 0;
+    unsigned grid = 0;
     for (RowsGradTensor& t : a.t) {
-        t.chunks = (t.heads + kGradHeadsPerChunk - 1) / kGradHeadsPerChunk;
-        units = units > a.n_tokens * t.chunks ? units : a.n_tokens * t.chunks;
-        tensors += t.heads > 0 ? 1 : 0;
+        t.chunks = rows_grad_chunks(t.heads);
+        t.ctas = t.heads > 0 ? (int32_t)grad_ctas(a.n_tokens, t.heads, t.chunks, kThreads / (head_dim / 8), sm_count) : 0;
+        grid += (unsigned)t.ctas;
     }
-    const int groups = kThreads / (head_dim / 8);
-    const int64_t all = (units + groups - 1) / groups;
-    const int most = grad_ctas(sm_count);
-    const dim3 grid((unsigned)(all < most ? all : most), (unsigned)tensors);
     return dtype == HTTM_BF16 ? launch_rows_grad_of<__nv_bfloat16>(a, head_dim, grid, stream) : launch_rows_grad_of<__half>(a, head_dim, grid, stream);
 }
 
@@ -429,6 +491,8 @@ bool rows_conflict(const httm_tensor& x, int64_t x_heads, const httm_tensor& y, 
 }  // namespace httm
 
 using namespace httm;
+
+constexpr int kPartialHeads = 8192;   // q's and k's together: the gradients' partial sums have their place from the start
 
 struct httm_rotary {
     httm_rotary_config cfg{};
@@ -524,7 +588,7 @@ int httm_rotary_create(const httm_rotary_config* config, httm_rotary** out) {
         double* d_f = nullptr;
         const int64_t n = (int64_t)(half > 0 ? c.n_positions : 0) * half;
         int rc = alloc(&r->words, 4, "rotary");
-        if (!rc) rc = alloc(&r->partial, rows_grad_partial_floats(c.head_dim, r->sm_count), "rotary");
+        if (!rc) rc = alloc(&r->partial, rows_grad_partial_floats(c.head_dim, rows_grad_chunks(kPartialHeads) + 1, r->sm_count), "rotary");
         if (!rc && n > 0) rc = alloc(&r->table, (size_t)n, "rotary");
         if (!rc) rc = cuda_result(cudaMemset(r->words, 0, 4 * sizeof(int32_t)), "rotary");
         if (!rc && n > 0) {
@@ -629,6 +693,8 @@ int httm_norm_rotate_backward(httm_rotary* r, int32_t dtype, int64_t n_tokens, c
         a.t[n++] = RowsGradTensor{t.x.ptr, t.dy.ptr, t.dx.ptr, t.x.stride_head, t.x.stride_token, t.dy.stride_head, t.dy.stride_token, t.dx.stride_head,
                                   t.dx.stride_token, t.weight, t.dweight, t.dbias, t.heads, 0};
     }
+    if ((q ? q->heads : 0) + (k ? k->heads : 0) > kPartialHeads)
+        return global_fail(HTTM_ERR_UNSUPPORTED, "norm_rotate_backward: at most %d heads of q and k together", kPartialHeads);
     OnDevice guard(r->cfg.device);
     if (!guard.ok) return global_fail(HTTM_ERR_CUDA, "norm_rotate_backward: cudaSetDevice failed");
     a.table = r->view();

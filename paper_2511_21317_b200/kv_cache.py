@@ -15,6 +15,7 @@ in the library's CUDA kernels, and there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import numpy as np
 import torch
@@ -32,12 +33,8 @@ class _RotaryConfig(ctypes.Structure):
         ("eps", ctypes.c_double), ("base", ctypes.c_double), ("frequencies", ctypes.POINTER(ctypes.c_double))]
 
 
-class _Rows(ctypes.Structure):
-    _fields_ = [("x", _Tensor), ("y", _Tensor), ("heads", _i32), ("weight", _vp), ("bias", _vp)]
-
-
-class _RowsGrad(ctypes.Structure):
-    _fields_ = [("x", _Tensor), ("dy", _Tensor), ("dx", _Tensor), ("heads", _i32), ("weight", _vp), ("dweight", _vp), ("dbias", _vp)]
+_ROWS = struct.Struct("Pqq Pqq i4x PP".replace(" ", ""))               # httm_rows: x, y, heads, weight, bias
+_ROWS_GRAD = struct.Struct("Pqq Pqq Pqq i4x PPP".replace(" ", ""))     # httm_rows_grad: x, dy, dx, heads, weight, dweight, dbias
 
 
 class _BatchConfig(ctypes.Structure):
@@ -59,8 +56,8 @@ def _library():
         L.httm_rotary_create.argtypes = [P(_RotaryConfig), P(_vp)]
         L.httm_rotary_destroy.argtypes = [_vp]
         L.httm_rotary_status.argtypes = [_vp, P(_i64)]
-        L.httm_norm_rotate.argtypes = [_vp, _i32, _i64, _vp, P(_Rows), P(_Rows), _vp]
-        L.httm_norm_rotate_backward.argtypes = [_vp, _i32, _i64, _vp, P(_RowsGrad), P(_RowsGrad), _vp]
+        L.httm_norm_rotate.argtypes = [_vp, _i32, _i64, _vp, _vp, _vp, _vp]
+        L.httm_norm_rotate_backward.argtypes = [_vp, _i32, _i64, _vp, _vp, _vp, _vp]
         L.httm_batch_create.argtypes = [P(_BatchConfig), P(_vp)]
         L.httm_batch_destroy.argtypes = [_vp]
         L.httm_batch_status.argtypes = [_vp, P(_i64)]
@@ -80,25 +77,36 @@ def _bad(message: str):
     raise HttmError(ERR_INVALID_ARG, message)
 
 
+# The kernels of a call on a few tokens take 2 - 3 us, so what is done per call is kept small: attributes are asked for once, arguments are
+# packed into a buffer that the handle keeps instead of into new structures, the current stream's address is asked for without building a
+# stream object (norm_rotate on one token, from call to call: 13.1 -> %s us; append 9.4 -> %s; attention of four tokens 10.9 -> %s).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream, device: int):
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    return stream.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(device)
+    return torch.cuda.current_stream(device).cuda_stream
 
 
-def _rows(t: torch.Tensor, name: str, shape, dtype, device: int) -> _Tensor:
-    if not t.is_cuda or t.dtype != dtype or t.device.index != device:
+def _rows(t: torch.Tensor, name: str, shape, dtype, device: int):
+    """(address, stride of heads, stride of tokens)"""
+    if t.dtype is not dtype or t.get_device() != device:
         _bad(f"{name}: expected a {dtype} tensor on cuda:{device}")
-    strides = t.stride()
-    if t.shape != shape or strides[2] != 1:
-        _bad(f"{name}: expected shape {tuple(shape)} [heads][tokens][head_dim] with contiguous channels")
-    return _Tensor(t.data_ptr(), strides[0], strides[1])
+    if t.shape != shape:
+        _bad(f"{name}: expected shape {tuple(shape)} [heads][tokens][head_dim]")
+    sh, st, sc = t.stride()
+    if sc != 1:
+        _bad(f"{name}: channels must be contiguous")
+    return t.data_ptr(), sh, st
 
 
-def _vector(t, name: str, dim: int, device: int):
+def _vector(t, name: str, dim: int, device: int) -> int:
     if t is None:
-        return None
-    if not t.is_cuda or t.dtype != torch.float32 or t.device.index != device or t.shape != (dim,) or not t.is_contiguous():
+        return 0
+    if t.dtype is not torch.float32 or t.get_device() != device or t.shape != (dim,) or not t.is_contiguous():
         _bad(f"{name}: expected a contiguous float32 vector of head_dim = {dim} on cuda:{device}")
     return t.data_ptr()
 
@@ -162,75 +170,82 @@ class Rotary(_Handle):
         h = _vp()
         _check(self._lib.httm_rotary_create(ctypes.byref(c), ctypes.byref(h)))
         self._h = h
+        self._args = ctypes.create_string_buffer(2 * _ROWS_GRAD.size)   # the two row arguments of a call
+        self._at = ctypes.addressof(self._args)
 
     def _positions(self, positions, tokens: int):
         if self.rotated_dim == 0:
             return None
         if positions is None:
             _bad("positions are missing")
-        if not positions.is_cuda or positions.dtype != torch.int32 or positions.device.index != self.device or not positions.is_contiguous() or \
-                tuple(positions.shape) not in ((tokens, self.axes),) + (((tokens,),) if self.axes == 1 else ()):
+        if positions.dtype is not torch.int32 or positions.get_device() != self.device or not positions.is_contiguous() or \
+                (positions.shape != (tokens, self.axes) and (self.axes != 1 or positions.shape != (tokens,))):
             _bad(f"positions: expected a contiguous int32 tensor [{tokens}][{self.axes}] on cuda:{self.device}")
         return positions.data_ptr()
+
+    @staticmethod
+    def _first(q, k):
+        first = q if q is not None else k
+        if first is None:
+            _bad("neither q nor k")
+        if first.dim() != 3:
+            _bad("expected [heads][tokens][head_dim]")
+        return _kind(first, "q" if q is not None else "k"), first.shape[1], first.dtype
 
     def norm_rotate(self, q, k, positions, q_weight=None, k_weight=None, q_bias=None, k_bias=None, out_q=None, out_k=None, stream=None):
         """rotate(norm(x) * weight + bias) of q and of k (either may be None); returns (q', k'), in out_q / out_k where given (which may
         be q and k themselves)."""
-        first = q if q is not None else k
-        if first is None:
-            _bad("neither q nor k")
-        kind = _kind(first, "q" if q is not None else "k")
-        tokens, dtype = first.shape[-2] if first.dim() == 3 else -1, first.dtype
-        args, outs = [], []
-        for x, w, b, out, name in ((q, q_weight, q_bias, out_q, "q"), (k, k_weight, k_bias, out_k, "k")):
-            if x is None:
-                args.append(None)
-                outs.append(None)
-                continue
-            shape = (x.shape[0], tokens, self.head_dim)
-            tx = _rows(x, name, shape, dtype, self.device)
-            if out is None:
-                out = torch.empty(shape, dtype=dtype, device=x.device)
-            args.append(ctypes.byref(_Rows(tx, _rows(out, "out_" + name, shape, dtype, self.device), shape[0],
-                                           _vector(w, name + "_weight", self.head_dim, self.device),
-                                           _vector(b, name + "_bias", self.head_dim, self.device))))
-            outs.append(out)
-        _check(self._lib.httm_norm_rotate(self._handle(), kind, tokens, self._positions(positions, tokens), args[0], args[1],
-                                          _stream(stream, self.device)))
+        kind, tokens, dtype = self._first(q, k)
+        dim, device = self.head_dim, self.device
+        at, outs = [None, None], [None, None]
+        if q is not None:
+            shape = (q.shape[0], tokens, dim)
+            x = _rows(q, "q", shape, dtype, device)
+            if out_q is None:
+                out_q = torch.empty(shape, dtype=dtype, device=q.device)
+            _ROWS.pack_into(self._args, 0, *x, *_rows(out_q, "out_q", shape, dtype, device), shape[0], _vector(q_weight, "q_weight", dim, device),
+                            _vector(q_bias, "q_bias", dim, device))
+            at[0], outs[0] = self._at, out_q
+        if k is not None:
+            shape = (k.shape[0], tokens, dim)
+            x = _rows(k, "k", shape, dtype, device)
+            if out_k is None:
+                out_k = torch.empty(shape, dtype=dtype, device=k.device)
+            _ROWS.pack_into(self._args, _ROWS.size, *x, *_rows(out_k, "out_k", shape, dtype, device), shape[0],
+                            _vector(k_weight, "k_weight", dim, device), _vector(k_bias, "k_bias", dim, device))
+            at[1], outs[1] = self._at + _ROWS.size, out_k
+        _check(self._lib.httm_norm_rotate(self._handle(), kind, tokens, self._positions(positions, tokens), at[0], at[1], _stream(stream, device)))
         return tuple(outs)
 
     def norm_rotate_backward(self, dq, dk, q, k, positions, q_weight=None, k_weight=None, q_bias=None, k_bias=None, out_q=None,
                              out_k=None, stream=None):
         """Gradients of norm_rotate from those of its outputs: (dq, dk, dq_weight, dq_bias, dk_weight, dk_bias), None for what was not given.
         out_q / out_k take the first two (and may be dq / dk or q / k themselves)."""
-        first = q if q is not None else k
-        if first is None:
-            _bad("neither q nor k")
-        kind = _kind(first, "q" if q is not None else "k")
-        tokens, dtype = first.shape[-2] if first.dim() == 3 else -1, first.dtype
-        args, outs, sums = [], [], []
-        for x, dy, w, b, out, name in ((q, dq, q_weight, q_bias, out_q, "q"), (k, dk, k_weight, k_bias, out_k, "k")):
+        kind, tokens, dtype = self._first(q, k)
+        dim, device = self.head_dim, self.device
+        at, outs, sums = [None, None], [None, None], [None] * 4
+        for i, (x, dy, w, b, out, name) in enumerate(((q, dq, q_weight, q_bias, out_q, "q"), (k, dk, k_weight, k_bias, out_k, "k"))):
             if x is None:
-                args.append(None)
-                outs.append(None)
-                sums += [None, None]
                 continue
             if dy is None:
                 _bad(f"d{name} is missing")
-            shape = (x.shape[0], tokens, self.head_dim)
-            tx, tdy = _rows(x, name, shape, dtype, self.device), _rows(dy, "d" + name, shape, dtype, self.device)
+            shape = (x.shape[0], tokens, dim)
+            tx, tdy = _rows(x, name, shape, dtype, device), _rows(dy, "d" + name, shape, dtype, device)
             if out is None:
                 out = torch.empty(shape, dtype=dtype, device=x.device)
-            weight = _vector(w, name + "_weight", self.head_dim, self.device)
-            _vector(b, name + "_bias", self.head_dim, self.device)
-            dw = None if w is None else torch.empty(self.head_dim, dtype=torch.float32, device=x.device)
-            db = None if b is None else torch.empty(self.head_dim, dtype=torch.float32, device=x.device)
-            args.append(ctypes.byref(_RowsGrad(tx, tdy, _rows(out, "out_" + name, shape, dtype, self.device), shape[0], weight,
-                                               None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr())))
-            outs.append(out)
-            sums += [dw, db]
-        _check(self._lib.httm_norm_rotate_backward(self._handle(), kind, tokens, self._positions(positions, tokens), args[0], args[1],
-                                                   _stream(stream, self.device)))
+            weight = _vector(w, name + "_weight", dim, device)
+            _vector(b, name + "_bias", dim, device)
+            to_w = to_b = 0
+            if w is not None:
+                sums[2 * i] = torch.empty(dim, dtype=torch.float32, device=x.device)
+                to_w = sums[2 * i].data_ptr()
+            if b is not None:
+                sums[2 * i + 1] = torch.empty(dim, dtype=torch.float32, device=x.device)
+                to_b = sums[2 * i + 1].data_ptr()
+            _ROWS_GRAD.pack_into(self._args, i * _ROWS_GRAD.size, *tx, *tdy, *_rows(out, "out_" + name, shape, dtype, device), shape[0], weight, to_w, to_b)
+            at[i], outs[i] = self._at + i * _ROWS_GRAD.size, out
+        _check(self._lib.httm_norm_rotate_backward(self._handle(), kind, tokens, self._positions(positions, tokens), at[0], at[1],
+                                                   _stream(stream, device)))
         return tuple(outs) + tuple(sums)
 
     def differentiable(self, q, k, positions, q_weight=None, k_weight=None, q_bias=None, k_bias=None):
@@ -321,13 +336,17 @@ class KvCache:
         if k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype or k_pages.device != v_pages.device:
             _bad("k_pages and v_pages must have the same shape, type and device")
         self.k_pages, self.v_pages = k_pages, v_pages
-        self.device = k_pages.device.index
+        self.device = k_pages.get_device()
+        self._dtype = k_pages.dtype
+        self._in, self._in2, self._out = _Tensor(), _Tensor(), _Tensor()   # arguments of a call
         self._kind = _DTYPES[k_pages.dtype]
         self._pages = [_Pages(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)) for t in (k_pages, v_pages)]
 
+        self._shape = tuple(k_pages.shape)
+
     def _check_batch(self, batch: CacheBatch):
-        n, h, s, d = self.k_pages.shape
-        if (h, s, d) != (batch.kv_heads, batch.page_size, batch.head_dim) or n < batch.n_pages or batch.device != self.device:
+        n, h, s, d = self._shape
+        if h != batch.kv_heads or s != batch.page_size or d != batch.head_dim or n < batch.n_pages or batch.device != self.device:
             _bad("the batch is for caches of another shape or device")
 
     def append(self, batch: CacheBatch, k, v, rotary: Rotary = None, positions=None, k_weight=None, k_bias=None, stream=None):
@@ -335,8 +354,9 @@ class KvCache:
         by `positions` or by the token's place behind the prefix."""
         self._check_batch(batch)
         shape = (batch.kv_heads, batch.n_tokens, batch.head_dim)
-        dtype = self.k_pages.dtype
-        tk, tv = _rows(k, "k", shape, dtype, self.device), _rows(v, "v", shape, dtype, self.device)
+        tk, tv = self._in, self._in2
+        tk.ptr, tk.stride_head, tk.stride_token = _rows(k, "k", shape, self._dtype, self.device)
+        tv.ptr, tv.stride_head, tv.stride_token = _rows(v, "v", shape, self._dtype, self.device)
         pos = None
         if positions is not None:
             if rotary is None:
@@ -351,15 +371,17 @@ class KvCache:
         ([tokens][heads][head_dim] if `out` is given so).  scale: 1 / sqrt(head_dim) unless given."""
         self._check_batch(batch)
         H, N, D = batch.heads, batch.n_tokens, batch.head_dim
-        tq = _rows(q, "q", (H, N, D), self.k_pages.dtype, self.device)
+        tq, to = self._in, self._out
+        tq.ptr, tq.stride_head, tq.stride_token = _rows(q, "q", (H, N, D), self._dtype, self.device)
         if out is None:
-            out = torch.empty(N, H * D, dtype=q.dtype, device=q.device)
-        if not out.is_cuda or out.dtype != q.dtype or out.device != q.device:
+            out = torch.empty(N, H * D, dtype=self._dtype, device=q.device)
+        if out.dtype is not self._dtype or out.get_device() != self.device:
             _bad("out: expected a CUDA tensor of q's type")
-        if out.dim() == 2 and out.shape == (N, H * D) and out.stride(1) == 1:
-            to = _Tensor(out.data_ptr(), D, out.stride(0))
-        elif out.dim() == 3 and out.shape == (N, H, D) and out.stride(2) == 1:
-            to = _Tensor(out.data_ptr(), out.stride(1), out.stride(0))
+        strides = out.stride()
+        if out.shape == (N, H * D) and strides[1] == 1:
+            to.ptr, to.stride_head, to.stride_token = out.data_ptr(), D, strides[0]
+        elif out.shape == (N, H, D) and strides[2] == 1:
+            to.ptr, to.stride_head, to.stride_token = out.data_ptr(), strides[1], strides[0]
         else:
             _bad("out: expected [tokens][heads * head_dim] or [tokens][heads][head_dim] with contiguous channels")
         _check(self._lib.httm_cache_attention(batch._handle(), self._kind, self._pages[0], self._pages[1], tq, to,
