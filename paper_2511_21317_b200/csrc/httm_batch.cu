@@ -251,7 +251,6 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
     a.jobs = part_of<CacheJob>(b, b->at.narrow_jobs);
     a.job_start = part_of<int32_t>(b, b->at.narrow_start);
     a.table = part_of<int32_t>(b, b->at.table);
-    a.parts = part_of<int2>(b, b->at.parts);
     a.combine_tasks = part_of<CombineTask>(b, b->at.combine_tasks);
     a.q = q.ptr, a.k = k_pages.ptr, a.v = v_pages.ptr, a.out = out.ptr;
     a.q_head = q.stride_head, a.q_token = q.stride_token, a.out_head = out.stride_head, a.out_token = out.stride_token;
@@ -271,6 +270,7 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
         w.job_start = part_of<int32_t>(b, b->at.wide_start);
         rc = cuda_result(launch_cache_wide(w, c.head_dim, dtype, c.n_pages, (int)p.wide_start.size() - 1, stream), "cache_attention launch");
     }
+    a.early = !p.wide_jobs.empty();
     if (!rc && !p.narrow_jobs.empty()) rc = cuda_result(launch_cache_narrow(a, c.head_dim, dtype, (int)p.narrow_start.size() - 1, stream), "cache_attention launch");
     if (!rc && !p.combine_tasks.empty())
         rc = cuda_result(launch_cache_combine(a, c.head_dim, dtype, (int)p.combine_tasks.size(), stream), "cache_attention launch");

@@ -75,6 +75,10 @@ inline int narrow_tile(int64_t tokens, int group) {
     return 0;
 }
 
+// A prefix that more rows than this share goes to the wide kernel: on 64 rows the narrow one is bound by its matrix instructions (32 768 keys of 8 heads x 128
+// channels, 64 rows %s us narrow and %s wide).
+constexpr int kPrefixRows = 32;
+
 // What is to be dealt: a row tile (or a pair of them) and a key head, `tiles` key tiles.
 struct BatchItem {
     int32_t seg, head, pair, tiles;
@@ -255,7 +259,7 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     int32_t run0 = 0, run = 0;   // tokens of consecutive sequences that leave the prefix to common row tiles
     auto close_run = [&] {
         if (run > 0 && prefix > 0) {
-            const int one = narrow_tile(run, group), rows = one ? one : kWideRows, per = rows / group;
+            const int one = narrow_tile(run, group), rows = one && one <= kPrefixRows ? one : kWideRows, per = rows / group;
             for (int32_t t = 0; t < run; t += per) add(run0 + t, std::min<int32_t>(per, run - t), rows, prefix, -1, 0);
         }
         run = 0;
@@ -302,17 +306,34 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     d.kv_heads = c.kv_heads;
     d.deal(wide, sole, sm_count, 6, 4);
     d.collect(&p->wide_jobs, &p->wide_start);
-    d.deal(narrow, sole, 2 * sm_count, 2, 4);
+    d.deal(narrow, sole, narrow_ctas_per_sm(c.head_dim) * sm_count, 2, 4);
     d.collect(&p->narrow_jobs, &p->narrow_start);
     // rows whose keys were cut or lie in two row tiles; rows that see no key (they get zeros)
-    const int per_task = std::max(1, kCombineRows / group);
-    for (int32_t t = 0; t < p->n_tokens;) {
-        const int32_t a = p->prefix_seg[t], b = p->own_seg[t];
+    for (int32_t t = 0; t < p->n_tokens;) {   // tokens that lie in the same row tiles
+        const int32_t tiles[2] = {p->prefix_seg[t], p->own_seg[t]};
         int32_t n = 1;
-        while (n < per_task && t + n < p->n_tokens && p->prefix_seg[t + n] == a && p->own_seg[t + n] == b) ++n;
+        while (t + n < p->n_tokens && p->prefix_seg[t + n] == tiles[0] && p->own_seg[t + n] == tiles[1]) ++n;
         for (int h = 0; h < c.kv_heads; ++h) {
-            auto direct = [&](int32_t s) { return s >= 0 && p->parts[(size_t)s * c.kv_heads + h].y < 0; };
-            if (!direct(a) && !direct(b)) p->combine_tasks.push_back(CombineTask{t, n, a, b, h, {0, 0, 0}});
+            CombineTask task{};
+            task.head = h;
+            bool direct = false;
+            for (int k = 0; k < 2; ++k) {
+                if (tiles[k] < 0) continue;
+                const int2 parts = p->parts[(size_t)tiles[k] * c.kv_heads + h];
+                direct |= parts.y < 0;
+                task.unit[k] = parts.x, task.parts[k] = parts.y, task.tile_rows[k] = p->segs[tiles[k]].tile_rows;
+                task.row[k] = (t - p->segs[tiles[k]].token0) * group;
+            }
+            if (direct) continue;
+            task.row_room = kCombineRows;   // eight parts to a warp
+            while (task.row_room > 1 && (task.parts[0] + task.parts[1]) * task.row_room > 8 * kCombineWarps) task.row_room /= 2;
+            for (int32_t r = 0; r < n * group; r += task.row_room) {
+                CombineTask some = task;
+                some.token0 = t + r / group, some.first_head = r % group;
+                some.rows = std::min(task.row_room, n * group - r);
+                for (int k = 0; k < 2; ++k) some.row[k] += r;
+                p->combine_tasks.push_back(some);
+            }
         }
         t += n;
     }
@@ -320,7 +341,7 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
 
 // Where the parts of a plan lie in one block (offsets in bytes, multiples of 256).
 struct BatchLayout {
-    size_t segs = 0, narrow_jobs = 0, wide_jobs = 0, narrow_start = 0, wide_start = 0, table = 0, parts = 0, combine_tasks = 0, slots = 0, positions = 0, bytes = 0;
+    size_t segs = 0, narrow_jobs = 0, wide_jobs = 0, narrow_start = 0, wide_start = 0, table = 0, combine_tasks = 0, slots = 0, positions = 0, bytes = 0;
     BatchLayout() = default;
     explicit BatchLayout(const BatchPlan& p) {
         auto room = [&](size_t n) {
@@ -330,7 +351,7 @@ struct BatchLayout {
         };
         auto of = [&](const auto& v) { return room(v.size() * sizeof(v[0])); };
         segs = of(p.segs), narrow_jobs = of(p.narrow_jobs), wide_jobs = of(p.wide_jobs), narrow_start = of(p.narrow_start), wide_start = of(p.wide_start);
-        table = of(p.table), parts = of(p.parts), combine_tasks = of(p.combine_tasks), slots = of(p.slots), positions = of(p.positions);
+        table = of(p.table), combine_tasks = of(p.combine_tasks), slots = of(p.slots), positions = of(p.positions);
         bytes += 256;
     }
     void write(const BatchPlan& p, unsigned char* to) const {
@@ -338,7 +359,7 @@ struct BatchLayout {
             if (!v.empty()) memcpy(to + at, v.data(), v.size() * sizeof(v[0]));
         };
         put(segs, p.segs), put(narrow_jobs, p.narrow_jobs), put(wide_jobs, p.wide_jobs), put(narrow_start, p.narrow_start), put(wide_start, p.wide_start);
-        put(table, p.table), put(parts, p.parts), put(combine_tasks, p.combine_tasks), put(slots, p.slots), put(positions, p.positions);
+        put(table, p.table), put(combine_tasks, p.combine_tasks), put(slots, p.slots), put(positions, p.positions);
     }
 };
 

@@ -1,0 +1,47 @@
+// Device helpers of the attention over a paged cache.
+//
+// A kernel of this path starts while the one in front of it still runs (httm_launch.cuh).  The plan of the batch (jobs, row tiles, page numbers) was uploaded
+// before that one started (behind the upload a kernel starts only when it is complete), so it is read ahead of depend_wait: four trips to memory that the first
+// keys would otherwise wait for (behind a stream of keys that has emptied L2 they take a microsecond each).  What is read there comes from L2.
+// Like all kernels of the library these let their successor start only after their own wait.
+#pragma once
+
+#include <type_traits>
+
+#include "httm_cache.h"
+#include "httm_internal.h"
+#include "httm_launch.cuh"
+
+namespace httm {
+
+__device__ __forceinline__ uint32_t ld_l2(const void* p) {
+    uint32_t v;
+    asm volatile("ld.global.cg.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ int4 ld_l2_16(const void* p) {
+    int4 v;
+    asm volatile("ld.global.cg.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+template <typename R>
+__device__ __forceinline__ R ld_record(const R* p) {   // a job, a row tile, a task
+    static_assert(sizeof(R) % 16 == 0 && alignof(R) >= 16, "whole 16-byte words");
+    R r;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(R) / 16); ++i) reinterpret_cast<int4*>(&r)[i] = ld_l2_16(reinterpret_cast<const int4*>(p) + i);
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+}
+
+}  // namespace httm

@@ -95,6 +95,7 @@ bool rows_conflict(const httm_tensor& x, int64_t x_heads, const httm_tensor& y, 
 constexpr int kNarrowKeys = 64;    // keys of a tile of the narrow kernel
 constexpr int kWideKeys = 128;     // of the wide kernel
 constexpr int kWideRows = 128;     // query rows of a tile of the wide kernel; the narrow kernel has 16, 32 or 64
+inline int narrow_ctas_per_sm(int head_dim) { return head_dim == 64 ? 3 : 2; }
 constexpr int kPartUnit = 16;      // partial results are laid out in units of 16 rows of head_dim + 2 floats
 
 // A row tile and the keys its rows see.  Rows are (token, query head of the group), the group's heads of a token side by side.
@@ -114,19 +115,20 @@ struct alignas(16) CacheJob {   // key tiles [tile0, tile1) of a row tile: those
     int32_t part2;              // of the second row tile
     int32_t pad;
 };
-constexpr int kCombineRows = 8;
-struct alignas(16) CombineTask {   // rows of a few tokens and one key head whose partial results are to be added up
-    int32_t token0, tokens;
-    int32_t prefix_seg, own_seg;   // the row tiles that hold them, or -1
-    int32_t head;
-    int32_t pad[3];
+constexpr int kCombineWarps = 8, kCombineRows = 8;
+struct alignas(16) CombineTask {   // rows of one key head whose partial results are to be added up
+    int32_t token0, first_head;    // the first row: token, head of the group; the others follow, the group's heads of a token side by side
+    int32_t rows, row_room;        // at most row_room (1, 2, 4 or 8): the fewer, the more warps share a row's parts
+    int32_t head, pad[3];
+    // of the row tile that looks at the prefix, and of the one that looks at the own keys: first unit and number of the partial results, rows of the tile,
+    // this task's first row in it (0 parts: there is no such tile)
+    int32_t unit[2], parts[2], tile_rows[2], row[2];
 };
 struct CacheArgs {
     const CacheSeg* segs;
     const CacheJob* jobs;
     const int32_t* job_start;   // [CTAs + 1]
     const int32_t* table;       // pages of the prefix, then of every sequence
-    const int2* parts;          // [row tile][kv head]: first unit, number of partial results (-1: written by its job)
     const CombineTask* combine_tasks;
     const void *q, *k, *v;
     void* out;
@@ -135,6 +137,7 @@ struct CacheArgs {
     float* partial;
     float scale_log2;
     int32_t group, kv_heads, page_shift, n_tokens;
+    int32_t early;              // narrow: the kernel in front belongs to the same call, inputs may be read while it runs
     int32_t* status;
 };
 cudaError_t configure_cache_attention();

@@ -3,14 +3,10 @@
 // A row tile has the query rows (token, head of the group) that share a key head, up to 64 of them, and walks the keys in tiles of 64:
 //   s = scale q K^T,  m' = max(m, max s),  p = 2^(s - m'),  l = l 2^(m - m') + sum p,  O = O 2^(m - m') + p V   (scores in units of log2 e)
 // Few rows leave nothing to compute per byte (at 4 rows 4 operations a byte), so the kernel is a stream of K and V through shared memory: 16-byte
-// asynchronous copies three tiles deep, two CTAs per SM.  The products are done by warp-level matrix instructions of 16 rows; four warps share
+// asynchronous copies three tiles deep, two CTAs per SM (three for 64 channels).  The products are done by warp-level matrix instructions of 16 rows; four warps share
 // a tile of 16 rows by keys (16 keys each), one of 32 rows two by two, one of 64 by rows, and keep their own maxima and sums until the
 // job ends.  The weights p are rounded to the values' type for the product with V, as they enter the matrix instruction; the sum l takes them before.
-#include <type_traits>
-
-#include "httm_cache.h"
-#include "httm_internal.h"
-#include "httm_launch.cuh"
+#include "httm_cache.cuh"
 
 namespace httm {
 
@@ -52,27 +48,11 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-template <typename T>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    if constexpr (std::is_same<T, __half>::value) {
-        const __half2 v = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&v);
-    } else {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&v);
-    }
-}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t ld_global_u32(const void* p) {
-    uint32_t v;
-    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p));
-    return v;
-}
-
 // Byte of 16-byte piece `piece` of row `row` in a tile of rows of D values: pieces are exchanged within a row so that the eight rows a matrix
 // load takes at once lie in distinct banks.
 template <int D>
@@ -80,54 +60,104 @@ __device__ __forceinline__ uint32_t tile_at(int row, int piece) {
     return (uint32_t)(row * (D * 2) + ((piece ^ (row & 7)) << 4));
 }
 
-struct KeyTile {   // one tile of 64 keys
-    const int32_t* pages;
-    int key0, keys;      // its first key in the prefix / in the sequence, how many the tile has
-    bool own;
+// The CTA's jobs are one stream of key tiles: tiles of the next job are on their way while the last ones of a job are worked on.  Up to kRecords jobs at a time lie in
+// shared memory (a CTA that has more starts over with the next ones).  The page numbers of a tile are read one tile before its copies are issued.
+constexpr int kRecords = 16, kMergeChannels = 32;
+template <int D>
+struct Shared {
+    unsigned char stages[kStages][kStageBytes<D>];
+    float merge[4][16][kMergeChannels];   // [warp][row]
+    float2 stats[4][16];
+    CacheJob jobs[kRecords];
+    CacheSeg segs[kRecords];
 };
-__device__ __forceinline__ KeyTile key_tile(const CacheArgs& a, const CacheSeg& seg, int tile) {
-    const int n_prefix = (seg.prefix_keys + kNarrowKeys - 1) / kNarrowKeys;
-    KeyTile t;
-    t.own = tile >= n_prefix;
-    t.key0 = (t.own ? tile - n_prefix : tile) * kNarrowKeys;
-    t.keys = min(kNarrowKeys, (t.own ? seg.own_keys : seg.prefix_keys) - t.key0);
-    t.pages = a.table + (t.own ? seg.own_table : 0);
-    return t;
-}
-
 template <typename T, int D>
-__device__ __forceinline__ void fetch(const CacheArgs& a, const KeyTile& t, int head, uint32_t stage, int tid) {
-    constexpr int PIECES = D / 8, ROWS = kThreads / PIECES;   // rows that the CTA fetches at once
-    const int piece = tid % PIECES;
-    const T* k = static_cast<const T*>(a.k) + head * a.k_head + piece * 8;
-    const T* v = static_cast<const T*>(a.v) + head * a.v_head + piece * 8;
-    const int mask = (1 << a.page_shift) - 1;
-#pragma unroll
-    for (int i = 0; i < kNarrowKeys / ROWS; ++i) {
-        const int row = tid / PIECES + i * ROWS;
-        const bool valid = row < t.keys;
-        const int key = t.key0 + (valid ? row : 0);
-        const int64_t page = ld_global(t.pages + (key >> a.page_shift));
-        const uint32_t at = stage + tile_at<D>(row, piece);
-        copy16(at, k + page * a.k_page + (key & mask) * a.k_slot, valid);
-        copy16(at + kNarrowKeys * D * 2, v + page * a.v_page + (key & mask) * a.v_slot, valid);
+struct Stream {
+    static constexpr int PIECES = D / 8, ROWS = kThreads / PIECES, COUNT = kNarrowKeys / ROWS;   // 16-byte pieces of a row; rows that the CTA copies at once
+    const CacheArgs& a;
+    Shared<D>& sm;
+    uint32_t base;      // of the stages
+    int n_jobs, job = -1;   // the job whose tiles are being read ahead
+    int left = 0;           // its tiles behind the one at hand
+    int own_keys, own_table;
+    int issued = 0, used = 0;
+    // the tile that is fetched next: its keys, their pages
+    int32_t pages[4];
+    const int32_t* table;
+    int head, key0, end, keys = 0;   // end: keys of the prefix / of the sequence
+    bool more;                       // own keys follow
+    __device__ __forceinline__ Stream(const CacheArgs& a_, Shared<D>& sm_, int n) : a(a_), sm(sm_), base(smem_of(sm_.stages[0])), n_jobs(n) { look_ahead(); }
+    __device__ __forceinline__ void start() {
+        for (int i = 0; i < kStages - 1; ++i) {
+            fetch();
+            look_ahead();
+        }
     }
-}
+    // Called behind the work on a tile, so that the page numbers arrive while the CTA waits for its next tile.
+    __device__ __forceinline__ void look_ahead() {
+        if (left > 0) {
+            --left;
+            key0 += kNarrowKeys;
+            if (more && key0 >= end) key0 = 0, end = own_keys, table = a.table + own_table, more = false;
+        } else {
+            keys = 0;
+            if (++job >= n_jobs) return;
+            const int tile = sm.jobs[job].tile0, prefix = sm.segs[job].prefix_keys, n_prefix = (prefix + kNarrowKeys - 1) / kNarrowKeys;
+            left = sm.jobs[job].tile1 - tile - 1;
+            head = sm.jobs[job].head;
+            own_keys = sm.segs[job].own_keys, own_table = sm.segs[job].own_table;
+            more = tile < n_prefix;
+            key0 = (more ? tile : tile - n_prefix) * kNarrowKeys;
+            end = more ? prefix : own_keys;
+            table = a.table + (more ? 0 : own_table);
+        }
+        keys = min(kNarrowKeys, end - key0);
+        // this thread's rows are threadIdx / PIECES + i ROWS: a quarter of the tile (16 keys, the smallest page) is COUNT / 4 of them
+        const int row = ((int)threadIdx.x / PIECES) % 16;
+        pages[0] = (int32_t)ld_l2(table + ((key0 + min(row, keys - 1)) >> a.page_shift));
+        if (a.page_shift < 6) {
+#pragma unroll
+            for (int i = 1; i < 4; ++i) pages[i] = (int32_t)ld_l2(table + ((key0 + min(16 * i + row, keys - 1)) >> a.page_shift));
+        } else {
+            pages[1] = pages[2] = pages[3] = pages[0];
+        }
+    }
+    __device__ __forceinline__ void fetch() {
+        if (keys > 0) {
+            const int piece = threadIdx.x % PIECES, mask = (1 << a.page_shift) - 1;
+            const uint32_t stage = base + (issued % kStages) * kStageBytes<D>;
+            const T* k = static_cast<const T*>(a.k) + head * a.k_head + piece * 8;
+            const T* v = static_cast<const T*>(a.v) + head * a.v_head + piece * 8;
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const int row = (int)threadIdx.x / PIECES + i * ROWS;
+                const bool valid = row < keys;
+                const int64_t page = pages[i * ROWS / 16];
+                const int slot = (key0 + (valid ? row : 0)) & mask;
+                const uint32_t at = stage + tile_at<D>(row, piece);
+                copy16(at, k + page * a.k_page + slot * a.k_slot, valid);
+                copy16(at + kNarrowKeys * D * 2, v + page * a.v_page + slot * a.v_slot, valid);
+            }
+            ++issued;
+        }
+        copies_commit();
+    }
+    __device__ __forceinline__ uint32_t next() {   // the stage of the next tile, once it is there for everybody
+        copies_wait<kStages - 2>();
+        __syncthreads();   // (and everybody is done with the tile before it)
+        fetch();
+        return base + (used++ % kStages) * kStageBytes<D>;
+    }
+};
 
 // One job with a tile of 16 MT rows.  Warp w has rows 16 (w mod MT) .. and of every key tile the keys 16 MT (w / MT) .. .
 template <typename T, int D, int MT>
-__device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg& seg, const CacheJob& job, unsigned char* smem) {
+__device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg seg, const CacheJob job, Shared<D>& sm, Stream<T, D>& stream) {
     constexpr int KG = 4 / MT, NB = 2 * MT;   // warps that share a row by keys; blocks of eight keys of a warp
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int row0 = (warp % MT) * 16 + (lane >> 2), key_base = (warp / MT) * 16 * MT;
     const int n_rows = seg.tokens * a.group;
-    const uint32_t base = smem_of(smem);
-    const int n = job.tile1 - job.tile0;
 
-    for (int i = 0; i < kStages - 1; ++i) {
-        if (i < n) fetch<T, D>(a, key_tile(a, seg, job.tile0 + i), job.head, base + i * kStageBytes<D>, tid);
-        copies_commit();
-    }
     // rows as operands of the matrix instruction: this thread has rows row0 and row0 + 8
     uint32_t qf[D / 16][4];
     int seen[2];   // own keys that the two rows see
@@ -141,8 +171,8 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg& s
                      2 * (lane & 3);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-            qf[c][r] = valid ? ld_global_u32(q + 16 * c) : 0u;
-            qf[c][2 + r] = valid ? ld_global_u32(q + 16 * c + 8) : 0u;
+            qf[c][r] = valid ? ld_l2(q + 16 * c) : 0u;
+            qf[c][2 + r] = valid ? ld_l2(q + 16 * c + 8) : 0u;
         }
     }
     float o[D / 8][4];
@@ -150,14 +180,11 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg& s
     for (int c = 0; c < D / 8; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
-    for (int i = 0; i < n; ++i) {
-        copies_wait<kStages - 2>();
-        __syncthreads();   // tile i is there for everybody, and everybody is done with tile i - 1
-        const int next = i + kStages - 1;
-        if (next < n) fetch<T, D>(a, key_tile(a, seg, job.tile0 + next), job.head, base + (next % kStages) * kStageBytes<D>, tid);
-        copies_commit();
-        const KeyTile t = key_tile(a, seg, job.tile0 + i);
-        const uint32_t ks = base + (i % kStages) * kStageBytes<D>, vs = ks + kNarrowKeys * D * 2;
+    const int n_prefix = (seg.prefix_keys + kNarrowKeys - 1) / kNarrowKeys;
+    for (int i = job.tile0; i < job.tile1; ++i) {
+        const uint32_t ks = stream.next(), vs = ks + kNarrowKeys * D * 2;
+        const bool own = i >= n_prefix;
+        const int key0 = (own ? i - n_prefix : i) * kNarrowKeys, keys = (own ? seg.own_keys : seg.prefix_keys) - key0;
         float s[NB][4];
 #pragma unroll
         for (int b = 0; b < NB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
@@ -174,7 +201,7 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg& s
         float top[2] = {-INFINITY, -INFINITY};
         int limit[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) limit[r] = t.own ? min(t.keys, seen[r] - t.key0) : t.keys;
+        for (int r = 0; r < 2; ++r) limit[r] = own ? min(keys, seen[r] - key0) : keys;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -217,182 +244,194 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg& s
                 mma<T>(o[2 * c + 1], pf, vf[2], vf[3]);
             }
         }
+        stream.look_ahead();
     }
     // the warps that share rows, added up in the order of their keys
-    copies_wait<0>();
-    __syncthreads();
-    float* all = reinterpret_cast<float*>(smem);                    // [warp][16][D]
-    float2* stats = reinterpret_cast<float2*>(smem + 4 * 16 * D * 4);   // [warp][16]
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-        const int at = warp * 16 + (lane >> 2) + 8 * r;
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c) *reinterpret_cast<float2*>(all + at * D + 8 * c + 2 * (lane & 3)) = make_float2(o[c][2 * r], o[c][2 * r + 1]);
-        if ((lane & 3) == 0) stats[at] = make_float2(m[r], l[r]);
+        if ((lane & 3) == 0) sm.stats[warp][(lane >> 2) + 8 * r] = make_float2(m[r], l[r]);
     }
-    __syncthreads();
-    constexpr int QUADS = D / 4;
-    for (int i = tid; i < n_rows * QUADS; i += kThreads) {
-        const int row = i / QUADS, c = i % QUADS;
-        float top = -INFINITY;
+    constexpr int QUADS = kMergeChannels / 4;
 #pragma unroll
-        for (int g = 0; g < KG; ++g) top = fmaxf(top, stats[(g * MT + row / 16) * 16 + row % 16].x);
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        float total = 0.f;
+    for (int c0 = 0; c0 < D; c0 += kMergeChannels) {
+        if (c0 > 0) __syncthreads();   // (the channels before these have been read; of the job before this one: the key tiles' barriers)
 #pragma unroll
-        for (int g = 0; g < KG; ++g) {
-            const int at = (g * MT + row / 16) * 16 + row % 16;
-            const float2 st = stats[at];
-            const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - top);
-            const float4 v = *reinterpret_cast<const float4*>(all + at * D + 4 * c);
-            sum.x = fmaf(v.x, f, sum.x), sum.y = fmaf(v.y, f, sum.y), sum.z = fmaf(v.z, f, sum.z), sum.w = fmaf(v.w, f, sum.w);
-            total = fmaf(st.y, f, total);
-        }
-        if (job.part < 0) {
-            const float inv = top == -INFINITY ? 0.f : 1.f / total;
-            T* out = static_cast<T*>(a.out) + (int64_t)(seg.token0 + row / a.group) * a.out_token + (int64_t)(job.head * a.group + row % a.group) * a.out_head + 4 * c;
-            *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum.x * inv, sum.y * inv), pack2<T>(sum.z * inv, sum.w * inv));
-        } else {
-            float* to = a.partial + (int64_t)job.part * (kPartUnit * (D + 2));
-            __stcg(reinterpret_cast<float4*>(to + row * D + 4 * c), sum);
-            if (c == 0) __stcg(reinterpret_cast<float2*>(to + 16 * MT * D + 2 * row), make_float2(top, total));
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int c = 0; c < kMergeChannels / 8; ++c)
+                *reinterpret_cast<float2*>(&sm.merge[warp][(lane >> 2) + 8 * r][8 * c + 2 * (lane & 3)]) = make_float2(o[c0 / 8 + c][2 * r], o[c0 / 8 + c][2 * r + 1]);
+        __syncthreads();
+        for (int i = tid; i < n_rows * QUADS; i += kThreads) {
+            const int row = i / QUADS, c = i % QUADS;
+            float top = -INFINITY;
+#pragma unroll
+            for (int g = 0; g < KG; ++g) top = fmaxf(top, sm.stats[g * MT + row / 16][row % 16].x);
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            float total = 0.f;
+#pragma unroll
+            for (int g = 0; g < KG; ++g) {
+                const float2 st = sm.stats[g * MT + row / 16][row % 16];
+                const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - top);
+                const float4 v = *reinterpret_cast<const float4*>(&sm.merge[g * MT + row / 16][row % 16][4 * c]);
+                sum.x = fmaf(v.x, f, sum.x), sum.y = fmaf(v.y, f, sum.y), sum.z = fmaf(v.z, f, sum.z), sum.w = fmaf(v.w, f, sum.w);
+                total = fmaf(st.y, f, total);
+            }
+            if (job.part < 0) {
+                const float inv = top == -INFINITY ? 0.f : 1.f / total;
+                T* out = static_cast<T*>(a.out) + (int64_t)(seg.token0 + row / a.group) * a.out_token + (int64_t)(job.head * a.group + row % a.group) * a.out_head +
+                         c0 + 4 * c;
+                *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum.x * inv, sum.y * inv), pack2<T>(sum.z * inv, sum.w * inv));
+            } else {
+                float* to = a.partial + (int64_t)job.part * (kPartUnit * (D + 2));
+                __stcg(reinterpret_cast<float4*>(to + row * D + c0 + 4 * c), sum);
+                if (c0 == 0 && c == 0) __stcg(reinterpret_cast<float2*>(to + 16 * MT * D + 2 * row), make_float2(top, total));
+            }
         }
     }
-    __syncthreads();   // the next job's copies go over what has been read here
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) cache_narrow_kernel(const __grid_constant__ CacheArgs a) {
-    extern __shared__ __align__(128) unsigned char smem[];
-    depend_wait();
-    dependents_launch();
-    const int last = ld_global(a.job_start + blockIdx.x + 1);
-    for (int j = ld_global(a.job_start + blockIdx.x); j < last; ++j) {
-        const CacheJob job = a.jobs[j];
-        const CacheSeg seg = a.segs[job.seg];
-        if (seg.tile_rows == 16)
-            narrow_job<T, D, 1>(a, seg, job, smem);
-        else if (seg.tile_rows == 32)
-            narrow_job<T, D, 2>(a, seg, job, smem);
-        else
-            narrow_job<T, D, 4>(a, seg, job, smem);
+__global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) cache_narrow_kernel(const __grid_constant__ CacheArgs a) {
+    extern __shared__ __align__(128) unsigned char smem_raw[];
+    Shared<D>& sm = *reinterpret_cast<Shared<D>*>(smem_raw);
+    const int last = (int)ld_l2(a.job_start + blockIdx.x + 1);
+    bool waited = false;
+    for (int j0 = (int)ld_l2(a.job_start + blockIdx.x); j0 < last; j0 += kRecords) {
+        const int n = min(kRecords, last - j0);
+        __syncthreads();   // (the records before these have been read)
+        if (threadIdx.x < 2 * n) {
+            const int j = threadIdx.x >> 1, half = threadIdx.x & 1;
+            const int4 v = ld_l2_16(reinterpret_cast<const int4*>(a.jobs + j0 + j) + half);
+            reinterpret_cast<int4*>(sm.jobs + j)[half] = v;
+            const int seg = __shfl_sync(__activemask(), v.x, threadIdx.x & 30);   // (the first word of a job)
+            reinterpret_cast<int4*>(sm.segs + j)[half] = ld_l2_16(reinterpret_cast<const int4*>(a.segs + seg) + half);
+        }
+        __syncthreads();
+        Stream<T, D> stream(a, sm, n);
+        if (!waited) {
+            if (!a.early) depend_wait();
+            dependents_launch();
+            waited = true;
+        }
+        stream.start();
+        for (int j = 0; j < n; ++j) {
+            const int rows = sm.segs[j].tile_rows;
+            if (rows == 16)
+                narrow_job<T, D, 1>(a, sm.segs[j], sm.jobs[j], sm, stream);
+            else if (rows == 32)
+                narrow_job<T, D, 2>(a, sm.segs[j], sm.jobs[j], sm, stream);
+            else
+                narrow_job<T, D, 4>(a, sm.segs[j], sm.jobs[j], sm, stream);
+        }
+        copies_wait<0>();
     }
+    if (a.early) depend_wait();   // whoever waits for this kernel means the one before it too
 }
 
-// The partial results of rows whose keys were shared out, added up in the order of the keys: out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m).  A CTA takes a few
-// rows; with fewer rows than warps the parts of a row are dealt to several warps, since a row of single tokens behind a long prefix has some
-// twenty parts and the time is that of the loads behind one another.  A row without parts gets zeros.
-constexpr int kCombineWarps = 8;
+// The partial results of rows whose keys were shared out, added up in the order of the keys: out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m).  A task is a few
+// rows, a CTA takes one, and all of its warps have something to add: a row of single tokens behind a long prefix has some forty parts, and the time is
+// that of the trips to L2 behind one another (values are asked for together with the maxima and sums that weight them).  A row without parts gets zeros.
+constexpr int kBatch = 8;   // parts that a warp asks for at a time
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const __grid_constant__ CacheArgs a) {
     constexpr int V = D / 32;   // channels of a lane
     __shared__ float4 shared_sum[kCombineWarps][32];
     __shared__ float2 shared_stat[kCombineWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const CombineTask task = ld_record(a.combine_tasks + blockIdx.x);
     depend_wait();
     dependents_launch();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const CombineTask task = a.combine_tasks[blockIdx.x];
-    const int rows = task.tokens * a.group;
-    int ways = 1;   // warps that share a row's parts
-    while (2 * ways * rows <= kCombineWarps) ways *= 2;
-    const int way = warp % ways;
-    // the parts of a tile lie one behind the other: n, the tile's rows, its first row of this task
-    int n0 = 0, n1 = 0, rows0 = 0, rows1 = 0, first0 = 0, first1 = 0;
-    const float *base0 = nullptr, *base1 = nullptr;
-    auto find = [&](int seg, int& n, int& tile_rows, int& first, const float*& base) {
-        if (seg < 0) return;
-        const int2 part = a.parts[(int64_t)seg * a.kv_heads + task.head];
-        const int4 s = *reinterpret_cast<const int4*>(a.segs + seg);   // token0, tokens, tile_rows
-        n = part.y;
-        tile_rows = s.z;
-        first = (task.token0 - s.x) * a.group;
-        base = a.partial + (int64_t)part.x * (kPartUnit * (D + 2));
-    };
-    find(task.prefix_seg, n0, rows0, first0, base0);
-    find(task.own_seg, n1, rows1, first1, base1);
-    const int n = n0 + n1;
-    for (int r0 = 0; r0 < rows; r0 += kCombineWarps / ways) {
-        const int row = r0 + warp / ways;
-        const bool here = row < rows;
-        // part p of the row: its values and its (maximum, sum)
-        auto values = [&](int p) {
-            return p < n0 ? base0 + (int64_t)p * rows0 * (D + 2) + (first0 + row) * D : base1 + (int64_t)(p - n0) * rows1 * (D + 2) + (first1 + row) * D;
-        };
-        auto stat = [&](int p) {
-            return p < n0 ? base0 + (int64_t)p * rows0 * (D + 2) + rows0 * D + 2 * (first0 + row)
-                          : base1 + (int64_t)(p - n0) * rows1 * (D + 2) + rows1 * D + 2 * (first1 + row);
-        };
-        float top = -INFINITY, total = 0.f, sum[V];
+    const int ways = kCombineWarps / kCombineRows * (kCombineRows / task.row_room);   // warps that share a row's parts
+    const int r = warp / ways, way = warp % ways;
+    const bool here = r < task.rows;
+    // the parts of a row tile lie one behind the other; those of the prefix come first
+    const int n0 = task.parts[0], n = n0 + task.parts[1];
+    const float* base[2];
+    int64_t stride[2];
+    int stat_at[2];   // of a part's (maximum, sum), from its values
 #pragma unroll
-        for (int c = 0; c < V; ++c) sum[c] = 0.f;
-        if (here) {
-            for (int p0 = way; p0 < n; p0 += 32 * ways) {   // 32 parts at a time, one per lane
-                const int mine = p0 + lane * ways;
-                float2 st = make_float2(-INFINITY, 0.f);
-                if (mine < n) st = __ldcg(reinterpret_cast<const float2*>(stat(mine)));
-                float high = st.x;
+    for (int k = 0; k < 2; ++k) {
+        const int row = task.row[k] + r;
+        stride[k] = (int64_t)task.tile_rows[k] * (D + 2);
+        base[k] = a.partial + (int64_t)task.unit[k] * (kPartUnit * (D + 2)) + row * D;
+        stat_at[k] = task.tile_rows[k] * D + 2 * row - row * D;
+    }
+    float top = -INFINITY, total = 0.f, sum[V];
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
-                const float to = fmaxf(top, high), shrink = top == -INFINITY ? 0.f : exp2_fast(top - to);
-                const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - to);
-                top = to;
-                total = fmaf(st.y, f, total * shrink);   // (a lane's share; added up below)
+    for (int c = 0; c < V; ++c) sum[c] = 0.f;
+    if (here) {
+        for (int p0 = way; p0 < n; p0 += kBatch * ways) {
+            float2 st[kBatch];
+            float v[kBatch][V];
 #pragma unroll
-                for (int c = 0; c < V; ++c) sum[c] *= shrink;
-                const int m = min(32, (n - p0 + ways - 1) / ways);
-#pragma unroll 8
-                for (int i = 0; i < m; ++i) {
-                    const float w = __shfl_sync(0xffffffffu, f, i);
-                    const float* at = values(p0 + i * ways) + lane * V;
+            for (int i = 0; i < kBatch; ++i) {
+                const int p = p0 + i * ways;
+                st[i] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[i][c] = 0.f;
+                if (p < n) {
+                    const float* at = p < n0 ? base[0] + p * stride[0] : base[1] + (p - n0) * stride[1];
+                    st[i] = __ldcg(reinterpret_cast<const float2*>(at + (p < n0 ? stat_at[0] : stat_at[1])));
                     if constexpr (V == 4) {
-                        const float4 v = __ldcg(reinterpret_cast<const float4*>(at));
-                        sum[0] = fmaf(v.x, w, sum[0]), sum[1] = fmaf(v.y, w, sum[1]), sum[2] = fmaf(v.z, w, sum[2]), sum[3] = fmaf(v.w, w, sum[3]);
+                        const float4 u = __ldcg(reinterpret_cast<const float4*>(at) + lane);
+                        v[i][0] = u.x, v[i][1] = u.y, v[i][2] = u.z, v[i][3] = u.w;
                     } else {
-                        const float2 v = __ldcg(reinterpret_cast<const float2*>(at));
-                        sum[0] = fmaf(v.x, w, sum[0]), sum[1] = fmaf(v.y, w, sum[1]);
+                        const float2 u = __ldcg(reinterpret_cast<const float2*>(at) + lane);
+                        v[i][0] = u.x, v[i][1] = u.y;
                     }
                 }
             }
+            float high = top;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-        }
-        if (ways > 1) {   // (one round of rows: rows * ways <= warps)
-            if constexpr (V == 4)
-                shared_sum[warp][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-            else
-                shared_sum[warp][lane] = make_float4(sum[0], sum[1], 0.f, 0.f);
-            if (lane == 0) shared_stat[warp] = make_float2(top, total);
-            __syncthreads();
-            if (way == 0) {
-                float high = top;
-                for (int i = 1; i < ways; ++i) high = fmaxf(high, shared_stat[warp + i].x);
-                const float own = top == -INFINITY ? 0.f : exp2_fast(top - high);
-                total *= own;
+            for (int i = 0; i < kBatch; ++i) high = fmaxf(high, st[i].x);
+            const float shrink = top == -INFINITY ? 0.f : exp2_fast(top - high);
+            top = high;
+            total *= shrink;
 #pragma unroll
-                for (int c = 0; c < V; ++c) sum[c] *= own;
-                for (int i = 1; i < ways; ++i) {
-                    const float2 st = shared_stat[warp + i];
-                    const float4 v = shared_sum[warp + i][lane];
-                    const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - high);
-                    total = fmaf(st.y, f, total);
-                    sum[0] = fmaf(v.x, f, sum[0]), sum[1] = fmaf(v.y, f, sum[1]);
-                    if constexpr (V == 4) sum[2] = fmaf(v.z, f, sum[2]), sum[3] = fmaf(v.w, f, sum[3]);
-                }
-                top = high;
+            for (int c = 0; c < V; ++c) sum[c] *= shrink;
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const float f = st[i].x == -INFINITY ? 0.f : exp2_fast(st[i].x - top);
+                total = fmaf(st[i].y, f, total);
+#pragma unroll
+                for (int c = 0; c < V; ++c) sum[c] = fmaf(v[i][c], f, sum[c]);
             }
         }
-        if (here && way == 0) {
-            const float inv = top == -INFINITY ? 0.f : 1.f / total;
-            const int token = task.token0 + row / a.group, head = task.head * a.group + row % a.group;
-            T* out = static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + lane * V;
-            if constexpr (V == 4)
-                *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum[0] * inv, sum[1] * inv), pack2<T>(sum[2] * inv, sum[3] * inv));
-            else
-                *reinterpret_cast<uint32_t*>(out) = pack2<T>(sum[0] * inv, sum[1] * inv);
-        }
     }
+    if (ways > 1) {
+        if constexpr (V == 4)
+            shared_sum[warp][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        else
+            shared_sum[warp][lane] = make_float4(sum[0], sum[1], 0.f, 0.f);
+        if (lane == 0) shared_stat[warp] = make_float2(top, total);
+        __syncthreads();
+        if (way != 0) return;
+        float high = top;
+        for (int i = 1; i < ways; ++i) high = fmaxf(high, shared_stat[warp + i].x);
+        const float own = top == -INFINITY ? 0.f : exp2_fast(top - high);
+        total *= own;
+#pragma unroll
+        for (int c = 0; c < V; ++c) sum[c] *= own;
+        for (int i = 1; i < ways; ++i) {
+            const float2 st = shared_stat[warp + i];
+            const float4 v = shared_sum[warp + i][lane];
+            const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - high);
+            total = fmaf(st.y, f, total);
+            sum[0] = fmaf(v.x, f, sum[0]), sum[1] = fmaf(v.y, f, sum[1]);
+            if constexpr (V == 4) sum[2] = fmaf(v.z, f, sum[2]), sum[3] = fmaf(v.w, f, sum[3]);
+        }
+        top = high;
+    }
+    if (!here) return;
+    const float inv = top == -INFINITY ? 0.f : 1.f / total;
+    const int at = task.first_head + r, token = task.token0 + at / a.group, head = task.head * a.group + at % a.group;
+    T* out = static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + lane * V;
+    if constexpr (V == 4)
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum[0] * inv, sum[1] * inv), pack2<T>(sum[2] * inv, sum[3] * inv));
+    else
+        *reinterpret_cast<uint32_t*>(out) = pack2<T>(sum[0] * inv, sum[1] * inv);
 }
 
 template <typename F>
@@ -401,7 +440,7 @@ cudaError_t allow_smem(F kernel, int bytes) {
 }
 template <typename T, int D>
 cudaError_t narrow_of(const CacheArgs& a, int ctas, cudaStream_t stream) {
-    return launch_kernel(cache_narrow_kernel<T, D>, ctas, kThreads, kStages * kStageBytes<D>, stream, a);
+    return launch_kernel(cache_narrow_kernel<T, D>, ctas, kThreads, sizeof(Shared<D>), stream, a);
 }
 template <typename T, int D>
 cudaError_t combine_of(const CacheArgs& a, int tasks, cudaStream_t stream) {
@@ -411,10 +450,10 @@ cudaError_t combine_of(const CacheArgs& a, int tasks, cudaStream_t stream) {
 }  // namespace
 
 cudaError_t configure_cache_attention() {
-    cudaError_t e = allow_smem(cache_narrow_kernel<__nv_bfloat16, 64>, kStages * kStageBytes<64>);
-    if (e == cudaSuccess) e = allow_smem(cache_narrow_kernel<__nv_bfloat16, 128>, kStages * kStageBytes<128>);
-    if (e == cudaSuccess) e = allow_smem(cache_narrow_kernel<__half, 64>, kStages * kStageBytes<64>);
-    if (e == cudaSuccess) e = allow_smem(cache_narrow_kernel<__half, 128>, kStages * kStageBytes<128>);
+    cudaError_t e = allow_smem(cache_narrow_kernel<__nv_bfloat16, 64>, sizeof(Shared<64>));
+    if (e == cudaSuccess) e = allow_smem(cache_narrow_kernel<__nv_bfloat16, 128>, sizeof(Shared<128>));
+    if (e == cudaSuccess) e = allow_smem(cache_narrow_kernel<__half, 64>, sizeof(Shared<64>));
+    if (e == cudaSuccess) e = allow_smem(cache_narrow_kernel<__half, 128>, sizeof(Shared<128>));
     return e;
 }
 

@@ -15,11 +15,7 @@
 //
 // A row's stabiliser is the largest score at the time it was set, and is raised only when a tile exceeds it by more than 2^8: weights of up to
 // 2^8 cost no precision (they are rounded relative to themselves, and sums are 32-bit), and raising it rewrites the accumulator.
-#include <type_traits>
-
-#include "httm_cache.h"
-#include "httm_internal.h"
-#include "httm_launch.cuh"
+#include "httm_cache.cuh"
 #include "tc_exp2.cuh"
 #include "tc_sm100.cuh"
 
@@ -56,16 +52,6 @@ struct Barriers {
     int abort_flag;
 };
 
-template <typename T>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    if constexpr (std::is_same<T, __half>::value) {
-        const __half2 v = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&v);
-    } else {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&v);
-    }
-}
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {   // not a number if one of them is not
     float d;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -139,13 +125,11 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         tc::prefetch_tensormap(&map_v);
     }
     if (warp == 1) tc::tmem_alloc(tc::smem_addr(&bars->tmem_base), kTmemColumns);
-    depend_wait();
-    dependents_launch();
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = bars->tmem_base;
-    const int job_first = ld_global(a.job_start + blockIdx.x), job_last = ld_global(a.job_start + blockIdx.x + 1);
+    const int job_first = (int)ld_l2(a.job_start + blockIdx.x), job_last = (int)ld_l2(a.job_start + blockIdx.x + 1);
 
     if (warp == 0 || warp == 10) {
         // ------------------------------------------------------------------ producers: Q and K (warp 0), V (warp 10)
@@ -162,22 +146,27 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         uint32_t loads[ST] = {}, q_loads = 0, tails = 0;   // completions that the loads issued so far bring to the barriers
         bool ok = true;
         for (int j = job_first; ok && j < job_last; ++j) {
-            const CacheJob job = a.jobs[j];
-            const CacheSeg seg = a.segs[job.seg + job.pair];   // (of a pair the second row tile sees the most keys)
+            const CacheJob job = ld_record(a.jobs + j);
+            const CacheSeg seg = ld_record(a.segs + job.seg + job.pair);   // (of a pair the second row tile sees the most keys)
+            const int token_a = job.pair ? seg.token0 - BM / a.group : seg.token0;
             const int n = job.tile1 - job.tile0;
             auto page_of = [&](int i) {   // of this lane's box of key tile i
                 const KeyTile t = key_tile(seg, job.tile0 + i);
                 const int p = lane / SUB;
-                return p * box < t.keys ? ld_global(a.table + t.table + (t.key0 >> a.page_shift) + p) : -1;
+                return p * box < t.keys ? (int32_t)ld_l2(a.table + t.table + (t.key0 >> a.page_shift) + p) : -1;
             };
             int32_t id = page_of(0);
+            if (j == job_first) {
+                depend_wait();
+                if (!is_v) dependents_launch();
+            }
             if (!is_v) {
                 if (q_loads > 0 && !(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->q_free), (q_loads - 1) & 1u, abort_flag)))) break;
                 if (lane == 0) {
                     tc::mbar_expect_tx(bar(bars->q_full), job.pair ? 2 * q_bytes : q_bytes);
                     for (int x = 0; x <= job.pair; ++x)
                         for (int c = 0; c < SUB; ++c)
-                            tma_load_4d(s_q + x * TILE + c * kSubTile, &map_q, bar(bars->q_full), 64 * c, 0, a.segs[job.seg + x].token0, job.head);
+                            tma_load_4d(s_q + x * TILE + c * kSubTile, &map_q, bar(bars->q_full), 64 * c, 0, job.pair && x == 0 ? token_a : seg.token0, job.head);
                 }
                 ++q_loads;
             }
@@ -311,7 +300,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             bool ok = true;
             int jobs = 0;
             for (int j = job_first; ok && j < job_last; ++j, ++jobs) {
-                const CacheJob job = a.jobs[j];
+                const CacheJob job = ld_record(a.jobs + j);
                 const int n = job.tile1 - job.tile0, n_score = job.pair ? 2 * n : n;
                 ok = tc::mbar_wait(bar(bars->q_full), (uint32_t)jobs & 1u, abort_flag);
                 if (!ok) break;
@@ -376,8 +365,9 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         bool ok = true;
         int jobs = 0;
         for (int jb = job_first; ok && jb < job_last; ++jb, ++jobs) {
-            const CacheJob job = a.jobs[jb];
-            const CacheSeg keys_seg = a.segs[job.seg + job.pair], seg = a.segs[job.seg + (job.pair ? x : 0)];
+            const CacheJob job = ld_record(a.jobs + jb);
+            const CacheSeg keys_seg = ld_record(a.segs + job.seg + job.pair), seg = ld_record(a.segs + job.seg + (job.pair ? x : 0));
+            if (jb == job_first) depend_wait();   // (partial results and `out` are free to be written)
             const int n = job.tile1 - job.tile0, n_score = job.pair ? 2 * n : n, n_own = job.pair ? n : (n - x + 1) / 2;
             const int token = row / a.group, head = job.head * a.group + row % a.group;
             const bool exists = token < seg.tokens;

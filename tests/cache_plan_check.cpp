@@ -97,7 +97,7 @@ static bool one_round() {
         const auto& jobs = wide ? p.wide_jobs : p.narrow_jobs;
         const auto& start = wide ? p.wide_start : p.narrow_start;
         if (jobs.empty()) continue;
-        NEED((int)start.size() - 1 <= (wide ? 1 : 2) * sms && start[0] == 0 && start.back() == (int)jobs.size());
+        NEED((int)start.size() - 1 <= (wide ? 1 : narrow_ctas_per_sm(c.head_dim)) * sms && start[0] == 0 && start.back() == (int)jobs.size());
         for (size_t i = 1; i < start.size(); ++i) NEED(start[i] > start[i - 1]);
         for (const CacheJob& j : jobs) {
             NEED(j.seg >= 0 && j.seg + j.pair < (int)p.segs.size() && j.head >= 0 && j.head < c.kv_heads && j.pair >= 0 && j.pair <= wide);
@@ -143,21 +143,29 @@ static bool one_round() {
         last = r.second;
     }
     // rows that are written by a job, and rows whose partial results are added up: every row exactly once
-    std::map<std::pair<int, int>, int> written;   // (token, head)
+    std::vector<int> written((size_t)tokens * c.heads, 0);   // (token, query head)
     for (const CombineTask& k : p.combine_tasks) {
-        NEED(k.tokens > 0 && k.token0 >= 0 && k.token0 + k.tokens <= tokens && k.head >= 0 && k.head < c.kv_heads);
-        for (int i = k.token0; i < k.token0 + k.tokens; ++i) {
-            NEED(p.prefix_seg[i] == k.prefix_seg && p.own_seg[i] == k.own_seg);
-            ++written[{i, k.head}];
+        NEED(k.rows > 0 && k.rows <= k.row_room && k.row_room <= kCombineRows && kCombineRows % k.row_room == 0);
+        NEED(k.first_head >= 0 && k.first_head < group && k.head >= 0 && k.head < c.kv_heads && k.token0 >= 0);
+        for (int r = 0; r < k.rows; ++r) {
+            const int i = k.token0 + (k.first_head + r) / group, g = (k.first_head + r) % group;
+            NEED(i < tokens);
+            for (int w = 0; w < 2; ++w) {
+                const int s = w ? p.own_seg[i] : p.prefix_seg[i];
+                NEED((s < 0) == (k.parts[w] == 0));
+                if (s < 0) continue;
+                const int2 parts = p.parts[(size_t)s * c.kv_heads + k.head];
+                NEED(k.unit[w] == parts.x && k.parts[w] == parts.y && parts.y > 0 && k.tile_rows[w] == p.segs[s].tile_rows);
+                NEED(k.row[w] + r == (i - p.segs[s].token0) * group + g && k.row[w] + r < k.tile_rows[w]);
+            }
+            ++written[(size_t)i * c.heads + k.head * group + g];
         }
-        for (int which : {k.prefix_seg, k.own_seg}) NEED(which < 0 || p.parts[(size_t)which * c.kv_heads + k.head].y > 0);
     }
     for (int s = 0; s < (int)p.segs.size(); ++s)
-        for (int h = 0; h < c.kv_heads; ++h)
-            if (p.parts[(size_t)s * c.kv_heads + h].y < 0)
-                for (int i = p.segs[s].token0; i < p.segs[s].token0 + p.segs[s].tokens; ++i) ++written[{i, h}];
-    NEED((int64_t)written.size() == (int64_t)tokens * c.kv_heads);
-    for (const auto& w : written) NEED(w.second == 1);
+        for (int h = 0; h < c.heads; ++h)
+            if (p.parts[(size_t)s * c.kv_heads + h / group].y < 0)
+                for (int i = p.segs[s].token0; i < p.segs[s].token0 + p.segs[s].tokens; ++i) ++written[(size_t)i * c.heads + h];
+    for (int w : written) NEED(w == 1);
     // the block of memory
     const BatchLayout at(p);
     std::vector<unsigned char> block(at.bytes, 0);
