@@ -325,12 +325,10 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
                 task.row[k] = (t - p->segs[tiles[k]].token0) * group;
             }
             if (direct) continue;
-            task.row_room = kCombineRows;   // eight parts to a warp
-            while (task.row_room > 1 && (task.parts[0] + task.parts[1]) * task.row_room > 8 * kCombineWarps) task.row_room /= 2;
-            for (int32_t r = 0; r < n * group; r += task.row_room) {
+            for (int32_t r = 0; r < n * group; r += kCombineRows) {
                 CombineTask some = task;
                 some.token0 = t + r / group, some.first_head = r % group;
-                some.rows = std::min(task.row_room, n * group - r);
+                some.rows = std::min(kCombineRows, n * group - r);
                 for (int k = 0; k < 2; ++k) some.row[k] += r;
                 p->combine_tasks.push_back(some);
             }

@@ -66,7 +66,7 @@ constexpr int kRecords = 16, kMergeChannels = 32;
 template <int D>
 struct Shared {
     unsigned char stages[kStages][kStageBytes<D>];
-    float merge[4][16][kMergeChannels];   // [warp][row]
+    float merge[4][16][kMergeChannels + 4];   // [warp][row]; the pitch keeps rows on distinct banks
     float2 stats[4][16];
     CacheJob jobs[kRecords];
     CacheSeg segs[kRecords];
@@ -263,8 +263,10 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg se
             for (int c = 0; c < kMergeChannels / 8; ++c)
                 *reinterpret_cast<float2*>(&sm.merge[warp][(lane >> 2) + 8 * r][8 * c + 2 * (lane & 3)]) = make_float2(o[c0 / 8 + c][2 * r], o[c0 / 8 + c][2 * r + 1]);
         __syncthreads();
-        for (int i = tid; i < n_rows * QUADS; i += kThreads) {
-            const int row = i / QUADS, c = i % QUADS;
+        for (int i = tid; i < 16 * MT * QUADS; i += kThreads) {
+            // the result is stored row by row, parts quad by quad (see cache_combine_kernel)
+            const int row = job.part < 0 ? i / QUADS : i % (16 * MT), c = job.part < 0 ? i % QUADS : i / (16 * MT);
+            if (row >= n_rows) continue;
             float top = -INFINITY;
 #pragma unroll
             for (int g = 0; g < KG; ++g) top = fmaxf(top, sm.stats[g * MT + row / 16][row % 16].x);
@@ -285,7 +287,7 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg se
                 *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum.x * inv, sum.y * inv), pack2<T>(sum.z * inv, sum.w * inv));
             } else {
                 float* to = a.partial + (int64_t)job.part * (kPartUnit * (D + 2));
-                __stcg(reinterpret_cast<float4*>(to + row * D + c0 + 4 * c), sum);
+                __stcg(reinterpret_cast<float4*>(to) + (c0 / 4 + c) * 16 * MT + row, sum);
                 if (c0 == 0 && c == 0) __stcg(reinterpret_cast<float2*>(to + 16 * MT * D + 2 * row), make_float2(top, total));
             }
         }
@@ -330,108 +332,93 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) cache_narrow_kernel
     if (a.early) depend_wait();   // whoever waits for this kernel means the one before it too
 }
 
-// The partial results of rows whose keys were shared out, added up in the order of the keys: out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m).  A task is a few
-// rows, a CTA takes one, and all of its warps have something to add: a row of single tokens behind a long prefix has some forty parts, and the time is
-// that of the trips to L2 behind one another (values are asked for together with the maxima and sums that weight them).  A row without parts gets zeros.
-constexpr int kBatch = 8;   // parts that a warp asks for at a time
+// The partial results of rows whose keys were shared out, added up in the order of the keys: out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m).  A part of a tile
+// of R rows is [D / 4][R] quads of channels and then [R] pairs (m, l): the thread of a row in the wide kernel writes with its neighbours whole lines (row
+// by row they were 32 half sectors per instruction, 4 600 .. 7 000 ns at the end of a job).  A CTA takes eight rows; its warps take the parts in turn, a lane
+// the quads q, q + 4, .. of one row, and the warps' sums meet in shared memory.  The time is that of trips to L2 behind one another, so values
+// are asked for together with the maxima that weight them.  A row without parts gets zeros.
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const __grid_constant__ CacheArgs a) {
-    constexpr int V = D / 32;   // channels of a lane
-    __shared__ float4 shared_sum[kCombineWarps][32];
-    __shared__ float2 shared_stat[kCombineWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int Q = D / 16, BATCH = 8 / Q * 2;   // quads of a lane; parts that it asks for at a time (4, or 2 for 128 channels)
+    __shared__ __align__(16) float sums[kCombineWarps][kCombineRows][D + 4];
+    __shared__ float2 stats[kCombineWarps][kCombineRows];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane & 7, quad = lane >> 3;
     const CombineTask task = ld_record(a.combine_tasks + blockIdx.x);
     depend_wait();
     dependents_launch();
-    const int ways = kCombineWarps / kCombineRows * (kCombineRows / task.row_room);   // warps that share a row's parts
-    const int r = warp / ways, way = warp % ways;
-    const bool here = r < task.rows;
-    // the parts of a row tile lie one behind the other; those of the prefix come first
-    const int n0 = task.parts[0], n = n0 + task.parts[1];
+    const int n0 = task.parts[0], n = n0 + task.parts[1];   // those of the prefix come first
     const float* base[2];
     int64_t stride[2];
-    int stat_at[2];   // of a part's (maximum, sum), from its values
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int row = task.row[k] + r;
+        base[k] = a.partial + (int64_t)task.unit[k] * (kPartUnit * (D + 2));
         stride[k] = (int64_t)task.tile_rows[k] * (D + 2);
-        base[k] = a.partial + (int64_t)task.unit[k] * (kPartUnit * (D + 2)) + row * D;
-        stat_at[k] = task.tile_rows[k] * D + 2 * row - row * D;
     }
-    float top = -INFINITY, total = 0.f, sum[V];
+    float top = -INFINITY, total = 0.f;
+    float4 sum[Q];
 #pragma unroll
-    for (int c = 0; c < V; ++c) sum[c] = 0.f;
-    if (here) {
-        for (int p0 = way; p0 < n; p0 += kBatch * ways) {
-            float2 st[kBatch];
-            float v[kBatch][V];
+    for (int c = 0; c < Q; ++c) sum[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row < task.rows) {
+        for (int p0 = warp; p0 < n; p0 += BATCH * kCombineWarps) {
+            float2 st[BATCH];
+            float4 v[BATCH][Q];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                const int p = p0 + i * ways;
+            for (int i = 0; i < BATCH; ++i) {
+                const int p = p0 + i * kCombineWarps;
                 st[i] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-                for (int c = 0; c < V; ++c) v[i][c] = 0.f;
+                for (int c = 0; c < Q; ++c) v[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (p < n) {
-                    const float* at = p < n0 ? base[0] + p * stride[0] : base[1] + (p - n0) * stride[1];
-                    st[i] = __ldcg(reinterpret_cast<const float2*>(at + (p < n0 ? stat_at[0] : stat_at[1])));
-                    if constexpr (V == 4) {
-                        const float4 u = __ldcg(reinterpret_cast<const float4*>(at) + lane);
-                        v[i][0] = u.x, v[i][1] = u.y, v[i][2] = u.z, v[i][3] = u.w;
-                    } else {
-                        const float2 u = __ldcg(reinterpret_cast<const float2*>(at) + lane);
-                        v[i][0] = u.x, v[i][1] = u.y;
-                    }
+                    const int k = p < n0 ? 0 : 1, tile_rows = task.tile_rows[k], at = task.row[k] + row;
+                    const float* part = base[k] + (p - (k ? n0 : 0)) * stride[k];
+                    st[i] = __ldcg(reinterpret_cast<const float2*>(part + tile_rows * D) + at);
+#pragma unroll
+                    for (int c = 0; c < Q; ++c) v[i][c] = __ldcg(reinterpret_cast<const float4*>(part) + (quad + 4 * c) * tile_rows + at);
                 }
             }
             float high = top;
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) high = fmaxf(high, st[i].x);
+            for (int i = 0; i < BATCH; ++i) high = fmaxf(high, st[i].x);
             const float shrink = top == -INFINITY ? 0.f : exp2_fast(top - high);
             top = high;
             total *= shrink;
 #pragma unroll
-            for (int c = 0; c < V; ++c) sum[c] *= shrink;
+            for (int c = 0; c < Q; ++c) sum[c].x *= shrink, sum[c].y *= shrink, sum[c].z *= shrink, sum[c].w *= shrink;
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
+            for (int i = 0; i < BATCH; ++i) {
                 const float f = st[i].x == -INFINITY ? 0.f : exp2_fast(st[i].x - top);
                 total = fmaf(st[i].y, f, total);
 #pragma unroll
-                for (int c = 0; c < V; ++c) sum[c] = fmaf(v[i][c], f, sum[c]);
+                for (int c = 0; c < Q; ++c)
+                    sum[c].x = fmaf(v[i][c].x, f, sum[c].x), sum[c].y = fmaf(v[i][c].y, f, sum[c].y), sum[c].z = fmaf(v[i][c].z, f, sum[c].z),
+                    sum[c].w = fmaf(v[i][c].w, f, sum[c].w);
             }
         }
-    }
-    if (ways > 1) {
-        if constexpr (V == 4)
-            shared_sum[warp][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-        else
-            shared_sum[warp][lane] = make_float4(sum[0], sum[1], 0.f, 0.f);
-        if (lane == 0) shared_stat[warp] = make_float2(top, total);
-        __syncthreads();
-        if (way != 0) return;
-        float high = top;
-        for (int i = 1; i < ways; ++i) high = fmaxf(high, shared_stat[warp + i].x);
-        const float own = top == -INFINITY ? 0.f : exp2_fast(top - high);
-        total *= own;
+        if (warp < n) {
 #pragma unroll
-        for (int c = 0; c < V; ++c) sum[c] *= own;
-        for (int i = 1; i < ways; ++i) {
-            const float2 st = shared_stat[warp + i];
-            const float4 v = shared_sum[warp + i][lane];
-            const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - high);
-            total = fmaf(st.y, f, total);
-            sum[0] = fmaf(v.x, f, sum[0]), sum[1] = fmaf(v.y, f, sum[1]);
-            if constexpr (V == 4) sum[2] = fmaf(v.z, f, sum[2]), sum[3] = fmaf(v.w, f, sum[3]);
+            for (int c = 0; c < Q; ++c) *reinterpret_cast<float4*>(&sums[warp][row][4 * (quad + 4 * c)]) = sum[c];
+            if (quad == 0) stats[warp][row] = make_float2(top, total);
         }
-        top = high;
     }
-    if (!here) return;
-    const float inv = top == -INFINITY ? 0.f : 1.f / total;
-    const int at = task.first_head + r, token = task.token0 + at / a.group, head = task.head * a.group + at % a.group;
-    T* out = static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + lane * V;
-    if constexpr (V == 4)
-        *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum[0] * inv, sum[1] * inv), pack2<T>(sum[2] * inv, sum[3] * inv));
-    else
-        *reinterpret_cast<uint32_t*>(out) = pack2<T>(sum[0] * inv, sum[1] * inv);
+    __syncthreads();
+    const int warps = min(n, kCombineWarps);
+    for (int i = threadIdx.x; i < task.rows * (D / 4); i += 32 * kCombineWarps) {
+        const int r = i / (D / 4), c = i % (D / 4);
+        float high = -INFINITY, l = 0.f;
+        for (int w = 0; w < warps; ++w) high = fmaxf(high, stats[w][r].x);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < warps; ++w) {
+            const float2 st = stats[w][r];
+            const float4 v = *reinterpret_cast<const float4*>(&sums[w][r][4 * c]);
+            const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - high);
+            l = fmaf(st.y, f, l);
+            o.x = fmaf(v.x, f, o.x), o.y = fmaf(v.y, f, o.y), o.z = fmaf(v.z, f, o.z), o.w = fmaf(v.w, f, o.w);
+        }
+        const float inv = high == -INFINITY ? 0.f : 1.f / l;
+        const int at = task.first_head + r, token = task.token0 + at / a.group, head = task.head * a.group + at % a.group;
+        T* out = static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + 4 * c;
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
+    }
 }
 
 template <typename F>

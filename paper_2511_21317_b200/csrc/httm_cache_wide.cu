@@ -513,7 +513,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     } else {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            __stcg(reinterpret_cast<float4*>(to + (int64_t)row * D + c + 4 * i),
+                            __stcg(reinterpret_cast<float4*>(to) + (c / 4 + i) * BM + row,
                                    make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3])));
                     }
                 }
