@@ -304,9 +304,9 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     Dealer d;
     d.p = p;
     d.kv_heads = c.kv_heads;
-    d.deal(wide, sole, sm_count, 6, 4);
+    d.deal(wide, sole, sm_count, 6, 2);
     d.collect(&p->wide_jobs, &p->wide_start);
-    d.deal(narrow, sole, narrow_ctas_per_sm(c.head_dim) * sm_count, 2, 4);
+    d.deal(narrow, sole, narrow_ctas_per_sm(c.head_dim) * sm_count, 2, 2);
     d.collect(&p->narrow_jobs, &p->narrow_start);
     // rows whose keys were cut or lie in two row tiles; rows that see no key (they get zeros)
     for (int32_t t = 0; t < p->n_tokens;) {   // tokens that lie in the same row tiles

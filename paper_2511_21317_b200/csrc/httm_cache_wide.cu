@@ -360,18 +360,29 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const int x = (warp - 2) >> 2, row = (warp & 3) * 32 + lane;   // group; row of the tile = lane of tensor memory
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_o = tmem + NB * BN + x * D + lane_addr;
-        uint32_t sp_base[NB] = {}, od_base = 0, singles = 0;
+        const uint32_t s_full0 = bar(bars->s_full[0]), p_full0 = bar(bars->p_full[0]);
+        uint32_t sp_bits = 0, od_base = 0, singles = 0;   // before this job: parity of each score buffer's completions; the group's P V; singles
         float2* xch = reinterpret_cast<float2*>(smem + (2 + 2 * ST) * TILE + 512);
         bool ok = true;
         int jobs = 0;
         for (int jb = job_first; ok && jb < job_last; ++jb, ++jobs) {
-            const CacheJob job = ld_record(a.jobs + jb);
-            const CacheSeg keys_seg = ld_record(a.segs + job.seg + job.pair), seg = ld_record(a.segs + job.seg + (job.pair ? x : 0));
-            if (jb == job_first) depend_wait();   // (partial results and `out` are free to be written)
-            const int n = job.tile1 - job.tile0, n_score = job.pair ? 2 * n : n, n_own = job.pair ? n : (n - x + 1) / 2;
-            const int token = row / a.group, head = job.head * a.group + row % a.group;
-            const bool exists = token < seg.tokens;
-            const int seen = exists ? min(seg.own_keys, seg.seen0 + token * seg.seen_step) : 0;
+            // (few registers are left beside the scores: what only the job's end needs is read again there)
+            int n_score, n_own, tile0, n_prefix, prefix_keys, seen_to;
+            bool pair;
+            {
+                const CacheJob job = ld_record(a.jobs + jb);
+                const CacheSeg seg = ld_record(a.segs + job.seg + (job.pair ? x : 0));
+                if (jb == job_first) depend_wait();   // (partial results and `out` are free to be written)
+                const int n = job.tile1 - job.tile0, token = row / a.group;
+                pair = job.pair != 0;
+                n_score = pair ? 2 * n : n;
+                n_own = pair ? n : (n - x + 1) / 2;
+                tile0 = job.tile0;
+                prefix_keys = seg.prefix_keys;
+                n_prefix = (prefix_keys + BN - 1) / BN;
+                // own keys that the row sees, counted like the tiles: behind the prefix's last, which is filled up
+                seen_to = n_prefix * BN + (token < seg.tokens ? min(seg.own_keys, seg.seen0 + token * seg.seen_step) : 0);
+            }
             float m = -INFINITY, l = 0.f;
             {   // the accumulator starts at zero: every P V adds to it (ordered before the first arrival at p_full)
                 uint32_t z[32];
@@ -381,12 +392,15 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 for (int c = 0; c < D; c += 32) tc::tmem_st32(t_o + c, z);
                 if (n_own == 0) tc::tmem_wait_st();
             }
+            int buf = x, round = 0;   // score tile 2 j + x is in buffer `buf`, used for the `round`-th time in this job
             for (int j = 0; j < n_own; ++j) {
-                const int k = 2 * j + x, buf = k % NB;
                 const uint32_t t_s = tmem + buf * BN + lane_addr;
-                const KeyTile t = key_tile(keys_seg, job.tile0 + (job.pair ? j : k));
-                const int limit = t.own ? min(t.keys, seen - t.key0) : (seg.prefix_keys > 0 ? t.keys : 0);
-                if (!(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->s_full[buf]), (sp_base[buf] + (uint32_t)(k / NB)) & 1u, abort_flag)))) break;
+                const int tile = tile0 + (pair ? j : 2 * j + x);
+                const int limit = (tile < n_prefix ? prefix_keys : seen_to) - tile * BN;   // keys of the tile that the row sees
+                const uint32_t parity = ((sp_bits >> buf) + (uint32_t)round) & 1u, p_full = p_full0 + 8 * buf;
+                if (!(ok = __all_sync(0xffffffffu, tc::mbar_wait(s_full0 + 8 * buf, parity, abort_flag)))) break;
+                buf += 2;
+                if (buf >= NB) buf -= NB, ++round;
                 tc::fence_after_sync();
                 uint32_t s[BN];
 #pragma unroll
@@ -456,9 +470,9 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
                 tc::tmem_wait_st();
                 tc::fence_before_sync();
-                tc::mbar_arrive(bar(bars->p_full[buf]));
+                tc::mbar_arrive(p_full);
             }
-            if (ok && !job.pair && x == 1) {
+            if (ok && !pair && x == 1) {
                 // single, group B: this row's (maximum, sum); O_B stays in tensor memory until group A has read it
                 xch[row] = make_float2(m, l);
                 tc::fence_before_sync();
@@ -466,11 +480,11 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->x_done), singles & 1u, abort_flag));
             } else if (ok) {
                 ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->o_final), (uint32_t)jobs & 1u, abort_flag));
-                if (ok && !job.pair) ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->x_full), singles & 1u, abort_flag));
+                if (ok && !pair) ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->x_full), singles & 1u, abort_flag));
                 if (!ok) break;
                 tc::fence_after_sync();
                 float fa = 1.f, fb = 0.f;
-                if (!job.pair) {   // both groups' sums: O = O_A 2^(m_A - m) + O_B 2^(m_B - m)
+                if (!pair) {   // both groups' sums: O = O_A 2^(m_A - m) + O_B 2^(m_B - m)
                     const float2 pb = xch[row];
                     const float mm = fmaxf(m, pb.x);
                     fa = m == -INFINITY ? 0.f : exp2f(m - mm);
@@ -479,7 +493,10 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     l = l * fa + pb.y * fb;
                     m = mm;
                 }
-                const int part = x == 0 ? job.part : job.part2;
+                const CacheJob job = ld_record(a.jobs + jb);
+                const CacheSeg seg = ld_record(a.segs + job.seg + (pair ? x : 0));
+                const int part = x == 0 ? job.part : job.part2, token = row / a.group, head = job.head * a.group + row % a.group;
+                const bool exists = token < seg.tokens;
                 if (part < 0) {
                     const float inv = m == -INFINITY ? 0.f : 1.f / l;
                     fa *= inv;
@@ -494,7 +511,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     tc::tmem_wait_ld();
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fa);
-                    if (!job.pair) {
+                    if (!pair) {
                         uint32_t ob[32];
                         tc::tmem_ld32(t_o + D + c, ob);   // O_B lies behind O_A
                         tc::tmem_wait_ld();
@@ -518,15 +535,15 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                 }
                 if (exists && part >= 0) __stcg(reinterpret_cast<float2*>(to + BM * D + 2 * row), make_float2(m, l));
-                if (!job.pair) {
+                if (!pair) {
                     tc::fence_before_sync();
                     tc::mbar_arrive(bar(bars->x_done));
                 }
             }
             od_base += (uint32_t)n_own;
-            if (!job.pair) ++singles;
+            if (!pair) ++singles;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) sp_base[b] += uses<NB>(n_score, b);
+            for (int b = 0; b < NB; ++b) sp_bits ^= (uses<NB>(n_score, b) & 1u) << b;
         }
     }
     tc::fence_before_sync();
