@@ -223,7 +223,8 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         if (tc::elect_one()) {
             constexpr bool kHalf = std::is_same<T, __half>::value;
             constexpr uint32_t kTypes = (1u << 7) | (1u << 10);   // A and B are bf16; without these bits fp16
-            constexpr uint32_t idesc_qk = tc::idesc_bf16(BM, BN, false, false) & ~(kHalf ? kTypes : 0u);
+            // a negative scale turns the sign of Q in the product (bit 13), so that the largest product is the largest score
+            const uint32_t idesc_qk = (tc::idesc_bf16(BM, BN, false, false) & ~(kHalf ? kTypes : 0u)) | (a.scale_log2 < 0.f ? 1u << 13 : 0u);
             constexpr uint32_t idesc_pv = tc::idesc_bf16(BM, 64, false, true) & ~(kHalf ? kTypes : 0u);
             const uint64_t dq0 = tc::smem_desc_sw128(s_q), dk0 = tc::smem_desc_sw128(s_k), dv0 = tc::smem_desc_sw128(s_v);
             constexpr uint64_t kTileStep = TILE >> 4, kSubStep = kSubTile >> 4;   // descriptors count 16-byte units
@@ -363,6 +364,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const uint32_t s_full0 = bar(bars->s_full[0]), p_full0 = bar(bars->p_full[0]);
         uint32_t sp_bits = 0, od_base = 0, singles = 0;   // before this job: parity of each score buffer's completions; the group's P V; singles
         float2* xch = reinterpret_cast<float2*>(smem + (2 + 2 * ST) * TILE + 512);
+        const float c = fmaxf(fabsf(a.scale_log2), 1e-30f);   // (not 0: a masked score is -inf, and stays so)
         bool ok = true;
         int jobs = 0;
         for (int jb = job_first; ok && jb < job_last; ++jb, ++jobs) {
@@ -406,12 +408,6 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 #pragma unroll
                 for (int c = 0; c < BN; c += 32) tc::tmem_ld32(t_s + c, s + c);
                 tc::tmem_wait_ld();
-                float c = a.scale_log2;
-                if (!(c > 0.f)) {   // the largest product is not the largest score: scores are scaled first
-#pragma unroll
-                    for (int i = 0; i < BN; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * c);
-                    c = 1.f;
-                }
                 if (limit < BN) {
 #pragma unroll
                     for (int i = 0; i < BN; ++i)
