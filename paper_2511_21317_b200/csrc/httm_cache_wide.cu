@@ -7,7 +7,7 @@
 //   warp 1      issues the products S = Q K^T (operands in shared memory) and O += P V (P in tensor memory over its S, V from shared memory)
 //   warps 2-5   softmax of group A, one thread per row: S from tensor memory, weights back as pairs of 16 bits; warps 6-9 of group B
 // S(k + NB) is issued right behind P(k) V into the buffer that this frees.  Tensor memory: NB score buffers of 128 columns and two accumulators of D, 512
-// columns in all (NB = 3 for 64 channels, 2 for 128).  Shared memory: two Q tiles and rings of 6 (2 for 128 channels) stages, 224 (192) KB.
+// columns in all (NB = 3 for 64 channels, 2 for 128).  The rings have as many stages: 128 and 192 KB with the Q tiles.
 //
 // Q comes in boxes of (channels, heads of the group, tokens), so the rows of a tile are (token, head) whatever the group's size and the tensor's
 // strides; rows that a tile does not fill compute something that nobody stores.  Keys behind the end of the prefix or of a sequence are masked
@@ -27,22 +27,23 @@ constexpr int BM = kWideRows, BN = kWideKeys;
 constexpr int kThreads = 352;   // registers are granted per four warps: as many per thread as with twelve
 constexpr int kTmemColumns = 512;
 constexpr int kSubTile = BM * 128;   // 128 rows of 64 channels
-constexpr int kPColumn = 64;         // P (16-bit pairs, 64 columns) lies over the last 64 columns of its S
+constexpr int kPColumn = 0;          // P (16-bit pairs, 64 columns) lies over the first 64 columns of its S
 constexpr float kRaise = 8.f;        // in units of log2
+// Of every eight pairs of scores, those whose bit is set here take the polynomial (FMA pipe), the others the special-function unit.
+constexpr uint32_t kPolyPairs = 0x11;
 
 template <int D>
 struct Shape {
-    static constexpr int NB = D == 64 ? 3 : 2;    // score buffers
-    static constexpr int ST = D == 64 ? 6 : 2;    // stages of the rings of K and of V: NB, or 2 NB where there is room
+    static constexpr int NB = D == 64 ? 3 : 2;    // score buffers, and stages of the rings of K and of V
     static constexpr int SUB = D / 64;            // 64-channel parts of a tile
     static constexpr int TILE = SUB * kSubTile;
-    static constexpr int SMEM = (2 + 2 * ST) * TILE + 1024 /*alignment*/ + 512 /*barriers*/ + BM * 8 /*exchange*/;
+    static constexpr int SMEM = (2 + 2 * NB) * TILE + 1024 /*alignment*/ + 512 /*barriers*/ + BM * 8 /*exchange*/;
 };
 
-template <int NB, int ST>
+template <int NB>
 struct Barriers {
     uint64_t q_full, q_free;
-    uint64_t k_full[ST], k_empty[ST], v_full[ST], v_empty[ST];
+    uint64_t k_full[NB], k_empty[NB], v_full[NB], v_empty[NB];
     uint64_t v_tail;                 // a V tile that needs zeros has arrived
     uint64_t s_full[NB], p_full[NB];
     uint64_t o_done[2];              // one completion per P V of the group
@@ -88,12 +89,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ CacheArgs a) {
     using S = Shape<D>;
-    constexpr int NB = S::NB, ST = S::ST, SUB = S::SUB, TILE = S::TILE;
+    constexpr int NB = S::NB, SUB = S::SUB, TILE = S::TILE;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    const uint32_t s_q = tc::smem_addr(smem), s_k = s_q + 2 * TILE, s_v = s_k + ST * TILE;
-    using Bars = Barriers<NB, ST>;
-    Bars* bars = reinterpret_cast<Bars*>(smem + (2 + 2 * ST) * TILE);
+    const uint32_t s_q = tc::smem_addr(smem), s_k = s_q + 2 * TILE, s_v = s_k + NB * TILE;
+    using Bars = Barriers<NB>;
+    Bars* bars = reinterpret_cast<Bars*>(smem + (2 + 2 * NB) * TILE);
     static_assert(sizeof(Bars) <= 512, "the barriers have 512 bytes");
     volatile int* abort_flag = &bars->abort_flag;
     auto bar = [](const uint64_t& b) { return tc::smem_addr(&b); };
@@ -103,13 +104,11 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         bars->abort_flag = 0;
         tc::mbar_init(bar(bars->q_full), 1);
         tc::mbar_init(bar(bars->q_free), 1);
-        for (int i = 0; i < ST; ++i) {
+        for (int i = 0; i < NB; ++i) {
             tc::mbar_init(bar(bars->k_full[i]), 1);
             tc::mbar_init(bar(bars->k_empty[i]), 1);
             tc::mbar_init(bar(bars->v_full[i]), 1);
             tc::mbar_init(bar(bars->v_empty[i]), 1);
-        }
-        for (int i = 0; i < NB; ++i) {
             tc::mbar_init(bar(bars->s_full[i]), 1);
             tc::mbar_init(bar(bars->p_full[i]), BM);
         }
@@ -142,8 +141,8 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const uint32_t ring = is_v ? s_v : s_k;
         uint64_t *full = is_v ? bars->v_full : bars->k_full, *empty = is_v ? bars->v_empty : bars->k_empty;
         const CUtensorMap* map = is_v ? &map_v : &map_k;
-        uint32_t base[ST] = {};          // key tiles of earlier jobs in every stage
-        uint32_t loads[ST] = {}, q_loads = 0, tails = 0;   // completions that the loads issued so far bring to the barriers
+        uint32_t base[NB] = {};          // key tiles of earlier jobs in every stage
+        uint32_t loads[NB] = {}, q_loads = 0, tails = 0;   // completions that the loads issued so far bring to the barriers
         bool ok = true;
         for (int j = job_first; ok && j < job_last; ++j) {
             const CacheJob job = ld_record(a.jobs + j);
@@ -171,12 +170,12 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 ++q_loads;
             }
 #pragma unroll 1
-            for (int i0 = 0; ok && i0 < n; i0 += ST) {
+            for (int i0 = 0; ok && i0 < n; i0 += NB) {
 #pragma unroll
-                for (int st = 0; st < ST; ++st) {   // key tile i of the job goes to stage i mod ST
+                for (int st = 0; st < NB; ++st) {   // key tile i of the job goes to stage i mod NB
                     const int i = i0 + st;
                     if (!ok || i >= n) break;
-                    const uint32_t fill = base[st] + (uint32_t)(i0 / ST);
+                    const uint32_t fill = base[st] + (uint32_t)(i0 / NB);
                     const KeyTile t = key_tile(seg, job.tile0 + i);
                     const int boxes = (t.keys + box - 1) / box, slot = t.key0 & (page - 1);   // (pages of 256: one of two halves)
                     const bool tail = is_v && t.keys < BN;
@@ -194,7 +193,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     ++tails;
                     __syncwarp();
                     if (!(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->v_tail), (tails - 1) & 1u, abort_flag)))) break;
-                    unsigned char* rows = smem + (2 + ST + st) * TILE;
+                    unsigned char* rows = smem + (2 + NB + st) * TILE;
                     for (int c = 0; c < SUB; ++c)
                         for (int at = t.keys * 8 + lane; at < BN * 8; at += 32) *reinterpret_cast<uint4*>(rows + c * kSubTile + at * 16) = make_uint4(0u, 0u, 0u, 0u);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -203,7 +202,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 }
             }
 #pragma unroll
-            for (int st = 0; st < ST; ++st) base[st] += uses<ST>(n, st);
+            for (int st = 0; st < NB; ++st) base[st] += uses<NB>(n, st);
         }
         if (!ok) {   // somebody gave up: what is still on its way has to land before the CTA leaves
             if (lane == 0) {
@@ -214,7 +213,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 landed(bars->q_full, q_loads);
                 landed(bars->v_tail, tails);
 #pragma unroll
-                for (int st = 0; st < ST; ++st) landed(full[st], loads[st]);
+                for (int st = 0; st < NB; ++st) landed(full[st], loads[st]);
             }
             __syncwarp();
         }
@@ -247,20 +246,19 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     for (int k = 0; k < 8; ++k) tc::mma_ts_c<true>(t_o + 64 * c, t_p + 8 * k, dv + c * kSubStep + (uint64_t)(k * 128), idesc_pv);
             };
             // The steps below are unrolled over 2 NB score tiles, so that every operand is a base plus a compile-time offset (operands that are recomputed
-            // per instruction make the issue cost more than the product).  Score tile k of a pair is key tile k / 2 of row tile k mod 2, of a single key
-            // tile k; key tile t of the job lies in stage t mod ST.  With ST = 2 NB a pair's rounds alternate between the halves of the ring (`half`).
-            uint32_t kv_base[ST] = {}, sp_base[NB] = {};   // completions before this job: ring stages, score buffers
+            // per instruction make the issue cost more than the product), and over no more than that: this code shares the instruction caches with the
+            // softmax warps (twice as many stages and steps cost 5 % of a call on pairs alone, 20 % of one on pairs and singles).  Score tile k of a
+            // pair is key tile k / 2 of row tile k mod 2, of a single key tile k; key tile t of the job lies in stage t mod NB.
+            uint32_t kv_base[NB] = {}, sp_base[NB] = {};   // completions before this job: ring stages, score buffers
             auto k_full = [&](int st, uint32_t n) { return tc::mbar_wait(bar(bars->k_full[st]), n & 1u, abort_flag); };
             auto v_full = [&](int st, uint32_t n) { return tc::mbar_wait(bar(bars->v_full[st]), n & 1u, abort_flag); };
-            constexpr int HALVES = ST / NB;
-            // k0: first score tile of the round, r: round.  HALF: its half of the ring
-            auto step_pair = [&](auto c_c, auto half_c, int k0, uint32_t r, int n_score) -> bool {
-                constexpr int C = decltype(c_c)::value, HALF = decltype(half_c)::value;
-                constexpr int B = C % NB, X = C % 2, T0 = HALF * NB + (C >> 1), STAGE = T0 % ST;
-                constexpr int XN = (C + NB) % 2, TN = HALF * NB + ((C + NB) >> 1), STAGEN = TN % ST;   // score tile k + NB: the next in this buffer
+            // k0: first score tile of the round, a multiple of 2 NB; r: round
+            auto step_pair = [&](auto c_c, int k0, uint32_t r, int n_score) -> bool {
+                constexpr int C = decltype(c_c)::value;
+                constexpr int B = C % NB, X = C % 2, STAGE = (C >> 1) % NB;
+                constexpr int XN = (C + NB) % 2, TN = (C + NB) >> 1, STAGEN = TN % NB;   // score tile k + NB: the next in this buffer
                 const uint32_t t_buf = tmem + B * BN, t_o = tmem + NB * BN + X * D;
-                const uint32_t lap = r / HALVES;   // how often the job has been round the ring
-                if (X == 0 && !v_full(STAGE, kv_base[STAGE] + lap)) return false;
+                if (X == 0 && !v_full(STAGE, kv_base[STAGE] + r)) return false;
                 if (!tc::mbar_wait(bar(bars->p_full[B]), (sp_base[B] + (C / NB)) & 1u, abort_flag)) return false;
                 tc::fence_after_sync();
                 issue_pv(t_o, t_buf + kPColumn, dv0 + STAGE * kTileStep);
@@ -268,7 +266,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 if (X == 1) tc::mma_commit(bar(bars->v_empty[STAGE]));
                 if (k0 + C + NB < n_score) {
                     if (XN == 0) {
-                        if (!k_full(STAGEN, kv_base[STAGEN] + lap + (TN >= ST ? 1u : 0u))) return false;
+                        if (!k_full(STAGEN, kv_base[STAGEN] + r + (TN >= NB ? 1u : 0u))) return false;
                         tc::fence_after_sync();
                     }
                     issue_qk(t_buf, dq0 + XN * kTileStep, dk0 + STAGEN * kTileStep, bar(bars->s_full[B]));
@@ -277,23 +275,21 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 }
                 return true;
             };
-            auto step_single = [&](auto c_c, int k0, uint32_t r, int n_single) -> bool {
+            auto step_single = [&](auto c_c, int k0, int n_single) -> bool {   // (a round is 2 NB key tiles, twice round the ring)
                 constexpr int C = decltype(c_c)::value;
-                constexpr int B = C % NB, X = C % 2, STAGE = C % ST, STAGEN = (C + NB) % ST;
+                constexpr int B = C % NB, X = C % 2;
                 const uint32_t t_buf = tmem + B * BN, t_o = tmem + NB * BN + X * D;
-                // a round is 2 NB key tiles: once round the ring, or twice
-                const uint32_t lap = r * (2 / HALVES) + C / ST, lap_n = r * (2 / HALVES) + (C + NB) / ST;
-                if (!v_full(STAGE, kv_base[STAGE] + lap)) return false;
+                if (!v_full(B, kv_base[B] + C / NB)) return false;
                 if (!tc::mbar_wait(bar(bars->p_full[B]), (sp_base[B] + C / NB) & 1u, abort_flag)) return false;
                 tc::fence_after_sync();
-                issue_pv(t_o, t_buf + kPColumn, dv0 + STAGE * kTileStep);
+                issue_pv(t_o, t_buf + kPColumn, dv0 + B * kTileStep);
                 tc::mma_commit(bar(bars->o_done[X]));
-                tc::mma_commit(bar(bars->v_empty[STAGE]));
+                tc::mma_commit(bar(bars->v_empty[B]));
                 if (k0 + C + NB < n_single) {
-                    if (!k_full(STAGEN, kv_base[STAGEN] + lap_n)) return false;
+                    if (!k_full(B, kv_base[B] + C / NB + 1u)) return false;
                     tc::fence_after_sync();
-                    issue_qk(t_buf, dq0, dk0 + STAGEN * kTileStep, bar(bars->s_full[B]));
-                    tc::mma_commit(bar(bars->k_empty[STAGEN]));
+                    issue_qk(t_buf, dq0, dk0 + B * kTileStep, bar(bars->s_full[B]));
+                    tc::mma_commit(bar(bars->k_empty[B]));
                     if (k0 + C + NB + 1 == n_single) tc::mma_commit(bar(bars->q_free));
                 }
                 return true;
@@ -331,28 +327,19 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                 };
                 if (job.pair) {
-                    for (int k0 = 0; ok && k0 < n_score; k0 += 2 * NB, ++r) {
-                        all([&](auto c) {
-                            if (ok && k0 + decltype(c)::value < n_score) ok = step_pair(c, std::integral_constant<int, 0>{}, k0, r, n_score);
-                        });
-                        if constexpr (HALVES == 2) {
-                            k0 += 2 * NB, ++r;
-                            all([&](auto c) {
-                                if (ok && k0 + decltype(c)::value < n_score) ok = step_pair(c, std::integral_constant<int, 1>{}, k0, r, n_score);
-                            });
-                        }
-                    }
-                } else {
                     for (int k0 = 0; ok && k0 < n_score; k0 += 2 * NB, ++r)
                         all([&](auto c) {
-                            if (ok && k0 + decltype(c)::value < n_score) ok = step_single(c, k0, r, n_score);
+                            if (ok && k0 + decltype(c)::value < n_score) ok = step_pair(c, k0, r, n_score);
+                        });
+                } else {
+                    for (int k0 = 0; ok && k0 < n_score; k0 += 2 * NB)
+                        all([&](auto c) {
+                            if (ok && k0 + decltype(c)::value < n_score) ok = step_single(c, k0, n_score);
                         });
                 }
                 if (ok) tc::mma_commit(bar(bars->o_final));
 #pragma unroll
-                for (int b = 0; b < NB; ++b) sp_base[b] += uses<NB>(n_score, b);
-#pragma unroll
-                for (int st = 0; st < ST; ++st) kv_base[st] += uses<ST>(n, st);
+                for (int b = 0; b < NB; ++b) sp_base[b] += uses<NB>(n_score, b), kv_base[b] += uses<NB>(n, b);
             }
         }
         __syncwarp();
@@ -363,7 +350,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const uint32_t t_o = tmem + NB * BN + x * D + lane_addr;
         const uint32_t s_full0 = bar(bars->s_full[0]), p_full0 = bar(bars->p_full[0]);
         uint32_t sp_bits = 0, od_base = 0, singles = 0;   // before this job: parity of each score buffer's completions; the group's P V; singles
-        float2* xch = reinterpret_cast<float2*>(smem + (2 + 2 * ST) * TILE + 512);
+        float2* xch = reinterpret_cast<float2*>(smem + (2 + 2 * NB) * TILE + 512);
         const float c = fmaxf(fabsf(a.scale_log2), 1e-30f);   // (not 0: a masked score is -inf, and stays so)
         bool ok = true;
         int jobs = 0;
@@ -404,28 +391,38 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 buf += 2;
                 if (buf >= NB) buf -= NB, ++round;
                 tc::fence_after_sync();
-                uint32_t s[BN];
+                // What bounds this loop is the way of its instructions to the warps: they are at different places of it, and what does not stay in the
+                // instruction caches is fetched for each (a branch of 128 multiplications that was never taken cost 13 %; CTAs of the same work took 870
+                // .. 1 150 us).  Hence no code per score beside the maximum and the weights: a score that the row does not see becomes -inf in its
+                // place in tensor memory, and the scores are read twice, 32 at a time, instead of being kept.
+                if (__any_sync(0xffffffffu, limit < BN)) {
+#pragma unroll 1
+                    for (int at = 0; at < BN; at += 8) {
+                        uint32_t v[8];
+                        tc::tmem_ld8(t_s + at, v);
+                        tc::tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < BN; c += 32) tc::tmem_ld32(t_s + c, s + c);
-                tc::tmem_wait_ld();
-                if (limit < BN) {
-#pragma unroll
-                    for (int i = 0; i < BN; ++i)
-                        if (i >= limit) s[i] = 0xff800000u;
-                }
-                float top;
-                {   // four independent chains
-                    float t4[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        t4[q] = max3_nan(__uint_as_float(s[32 * q]), __uint_as_float(s[32 * q + 1]), __uint_as_float(s[32 * q + 2]));
-#pragma unroll
-                        for (int i = 3; i < 31; i += 2) t4[q] = max3_nan(t4[q], __uint_as_float(s[32 * q + i]), __uint_as_float(s[32 * q + i + 1]));
+                        for (int i = 0; i < 8; ++i)
+                            if (at + i >= limit) v[i] = 0xff800000u;
+                        tc::tmem_st8(t_s + at, v);
                     }
-                    t4[0] = max3_nan(t4[0], t4[1], __uint_as_float(s[31]));
-                    t4[2] = max3_nan(t4[2], t4[3], __uint_as_float(s[63]));
-                    top = max3_nan(max3_nan(t4[0], t4[2], __uint_as_float(s[95])), __uint_as_float(s[127]), -INFINITY) * c;
+                    tc::tmem_wait_st();
                 }
+                uint32_t v0[32], v1[32];
+                float top0 = -INFINITY, top1 = -INFINITY;   // not a number if one of the scores is not
+#pragma unroll
+                for (int at = 0; at < BN; at += 64) {
+                    tc::tmem_ld32(t_s + at, v0);
+                    tc::tmem_ld32(t_s + at + 32, v1);
+                    tc::tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        top0 = max3_nan(top0, __uint_as_float(v0[i]), __uint_as_float(v0[i + 1]));
+                        top1 = max3_nan(top1, __uint_as_float(v1[i]), __uint_as_float(v1[i + 1]));
+                    }
+                }
+                tc::tmem_ld32(t_s, v0);
+                const float top = max3_nan(top0, top1, -INFINITY) * c;
                 const bool raise = !(top <= m + kRaise);   // (also where top is not a number)
                 if (__any_sync(0xffffffffu, raise)) {
                     const float f = raise ? exp2f(m - top) : 1.f;
@@ -448,20 +445,32 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 const float from = m == -INFINITY ? 0.f : m;
                 const float2 c2 = make_float2(c, c), neg = make_float2(-from, -from);
                 float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+                auto weights = [&](const uint32_t (&v)[32], uint32_t to) {   // 32 scores -> 16 columns of P
 #pragma unroll
-                for (int cc = 0; cc < 8; ++cc) {
-                    uint32_t pk[8];
+                    for (int g = 0; g < 2; ++g) {
+                        uint32_t pk[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 u = tc::ffma2(make_float2(__uint_as_float(s[cc * 16 + 2 * i]), __uint_as_float(s[cc * 16 + 2 * i + 1])), c2, neg);
-                        const float2 e = make_float2(fast_exp2(u.x), fast_exp2(u.y));
-                        if (i & 1)
-                            sum1 = tc::fadd2(sum1, e);
-                        else
-                            sum0 = tc::fadd2(sum0, e);
-                        pk[i] = pack2<T>(e.x, e.y);
+                        for (int i = 0; i < 8; ++i) {
+                            const float2 u = tc::ffma2(make_float2(__uint_as_float(v[g * 16 + 2 * i]), __uint_as_float(v[g * 16 + 2 * i + 1])), c2, neg);
+                            const float2 e = (kPolyPairs >> i) & 1u ? exp2_poly2(u) : make_float2(fast_exp2(u.x), fast_exp2(u.y));
+                            if (i & 1)
+                                sum1 = tc::fadd2(sum1, e);
+                            else
+                                sum0 = tc::fadd2(sum0, e);
+                            pk[i] = pack2<T>(e.x, e.y);
+                        }
+                        tc::tmem_st8(to + g * 8, pk);
                     }
-                    tc::tmem_st8(t_s + kPColumn + cc * 8, pk);
+                };
+                tc::tmem_wait_ld();
+#pragma unroll
+                for (int at = 0; at < BN; at += 64) {   // (P covers columns whose scores have been read)
+                    tc::tmem_ld32(t_s + at + 32, v1);
+                    weights(v0, t_s + kPColumn + at / 2);
+                    tc::tmem_wait_ld();
+                    if (at == 0) tc::tmem_ld32(t_s + 64, v0);
+                    weights(v1, t_s + kPColumn + at / 2 + 16);
+                    tc::tmem_wait_ld();
                 }
                 l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
                 tc::tmem_wait_st();
