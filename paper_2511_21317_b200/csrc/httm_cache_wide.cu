@@ -395,16 +395,19 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 // instruction caches is fetched for each (a branch of 128 multiplications that was never taken cost 13 %; CTAs of the same work took 870
                 // .. 1 150 us).  Hence no code per score beside the maximum and the weights: a score that the row does not see becomes -inf in its
                 // place in tensor memory, and the scores are read twice, 32 at a time, instead of being kept.
-                if (__any_sync(0xffffffffu, limit < BN)) {
+                const int full = __reduce_min_sync(0xffffffffu, limit);   // keys that all rows of the warp see
+                if (full < BN) {
 #pragma unroll 1
-                    for (int at = 0; at < BN; at += 8) {
-                        uint32_t v[8];
+                    for (int at = max(full, 0) & ~15; at < BN; at += 16) {
+                        uint32_t v[16];
                         tc::tmem_ld8(t_s + at, v);
+                        tc::tmem_ld8(t_s + at + 8, v + 8);
                         tc::tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
+                        for (int i = 0; i < 16; ++i)
                             if (at + i >= limit) v[i] = 0xff800000u;
                         tc::tmem_st8(t_s + at, v);
+                        tc::tmem_st8(t_s + at + 8, v + 8);
                     }
                     tc::tmem_wait_st();
                 }
