@@ -76,7 +76,7 @@ inline int narrow_tile(int64_t tokens, int group) {
 }
 
 // A prefix that more rows than this share goes to the wide kernel: on 64 rows the narrow one is bound by its matrix instructions (32 768 keys of 8 heads x 128
-// channels, 64 rows %s us narrow and %s wide).
+// channels, 64 rows 53 us narrow and 44 wide).
 constexpr int kPrefixRows = 32;
 
 // What is to be dealt: a row tile (or a pair of them) and a key head, `tiles` key tiles.
