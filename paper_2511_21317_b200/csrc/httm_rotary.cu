@@ -154,6 +154,12 @@ __device__ __forceinline__ float row_sum(float v) {
     for (int o = 1; o < LANES; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+template <int LANES>
+__device__ __forceinline__ float2 row_sum2(float2 v) {
+#pragma unroll
+    for (int o = 1; o < LANES; o *= 2) v = tc::fadd2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+    return v;
+}
 __device__ __forceinline__ float sum8(const float2 (&x)[4]) {
     const float2 s = tc::fadd2(tc::fadd2(x[0], x[1]), tc::fadd2(x[2], x[3]));
     return s.x + s.y;
@@ -305,29 +311,37 @@ __global__ void __launch_bounds__(kThreads, 2) rows_grad_kernel(const __grid_con
             unpack4<T>(ring.read(stage, 2 * i + 1, ch.a), g);
             unpack4<T>(ring.read(stage, 2 * i + 1, ch.b), g + 2);
             if (ch.rotates && here) turn<true>(g, cs, a.table.interleaved != 0);
+            // Two rounds of sums over the row instead of four behind one another: those of x and u = g w, then, with the mean taken off x, those of
+            // x^2 and u x.  With k = r^2 mean(u x) the gradient is r (u - mean u - x k).
+            float2 u[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) u[c] = tc::fmul2(g[c], w[c]);
             float r = 1.f;
-            if (a.norm != HTTM_NORM_NONE) r = normalise<LANES>(x, a.norm, a.eps);
+            if (a.norm != HTTM_NORM_NONE) {
+                float mu = 0.f;
+                if (a.norm == HTTM_NORM_LAYER) {
+                    const float2 means = row_sum2<LANES>(make_float2(sum8(x), sum8(u)));
+                    const float mean = means.x * (-1.0f / D);
+                    mu = means.y * (-1.0f / D);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) x[c] = tc::fadd2(x[c], make_float2(mean, mean));
+                }
+                const float2 xx = tc::ffma2(x[3], x[3], tc::ffma2(x[2], x[2], tc::ffma2(x[1], x[1], tc::fmul2(x[0], x[0]))));
+                const float2 ux = tc::ffma2(u[3], x[3], tc::ffma2(u[2], x[2], tc::ffma2(u[1], x[1], tc::fmul2(u[0], x[0]))));
+                const float2 sums2 = row_sum2<LANES>(make_float2(xx.x + xx.y, ux.x + ux.y));
+                r = rsqrtf(fmaf(sums2.x, 1.0f / D, a.eps));
+                const float k = r * r * sums2.y * (-1.0f / D);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) u[c] = tc::fmul2(make_float2(r, r), tc::ffma2(x[c], make_float2(k, k), tc::fadd2(u[c], make_float2(mu, mu))));
+            }
             if (exists) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) dw[c] = tc::ffma2(g[c], x[c], dw[c]), db[c] = tc::fadd2(db[c], g[c]);
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) g[c] = tc::fmul2(g[c], w[c]);
-            if (a.norm != HTTM_NORM_NONE) {
-                const float2 ux = tc::ffma2(g[3], x[3], tc::ffma2(g[2], x[2], tc::ffma2(g[1], x[1], tc::fmul2(g[0], x[0]))));
-                const float mux = row_sum<LANES>(ux.x + ux.y) * (-1.0f / D);
-                if (a.norm == HTTM_NORM_LAYER) {
-                    const float mu = row_sum<LANES>(sum8(g)) * (-1.0f / D);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) g[c] = tc::fadd2(g[c], make_float2(mu, mu));
-                }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) g[c] = tc::fmul2(make_float2(r, r), tc::ffma2(x[c], make_float2(mux, mux), g[c]));
+                for (int c = 0; c < 4; ++c) dw[c] = tc::ffma2(tc::fmul2(g[c], make_float2(r, r)), x[c], dw[c]), db[c] = tc::fadd2(db[c], g[c]);
             }
             if (exists) {
                 T* dx = dxs + i * t.dx_head + token * t.dx_token;
-                *reinterpret_cast<uint2*>(dx + ch.a) = pack4<T>(g);
-                *reinterpret_cast<uint2*>(dx + ch.b) = pack4<T>(g + 2);
+                *reinterpret_cast<uint2*>(dx + ch.a) = pack4<T>(u);
+                *reinterpret_cast<uint2*>(dx + ch.b) = pack4<T>(u + 2);
             }
         }
         stage = stage == kStages - 1 ? 0 : stage + 1;
