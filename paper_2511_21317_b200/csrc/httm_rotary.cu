@@ -274,34 +274,40 @@ __global__ void __launch_bounds__(kThreads, 2) rows_grad_kernel(const __grid_con
     const Ring<LANES> ring(smem, lane);
     depend_wait();
     dependents_launch();
-    const T *xs = static_cast<const T*>(t.x) + h0 * t.x_head + 8 * lane, *dys = static_cast<const T*>(t.dy) + h0 * t.dy_head + 8 * lane;
-    T* dxs = static_cast<T*>(t.dx) + h0 * t.dx_head;
-    const int64_t step = (int64_t)(t.ctas / t.chunks) * GROUPS;
-    int64_t token = (int64_t)column * GROUPS + group;
-    auto fetch = [&](int stage, int64_t of) {
+    // (token numbers stay below 2^31 plus a few grids; addresses are carried along, each turn adds one stride to them)
+    const uint32_t n_tokens = (uint32_t)a.n_tokens, step = (uint32_t)(t.ctas / t.chunks) * GROUPS;
+    uint32_t token = (uint32_t)(column * GROUPS + group), fetched = token;
+    const T* x_at = static_cast<const T*>(t.x) + h0 * t.x_head + 8 * lane + (int64_t)token * t.x_token;
+    const T* dy_at = static_cast<const T*>(t.dy) + h0 * t.dy_head + 8 * lane + (int64_t)token * t.dy_token;
+    T* dx_at = static_cast<T*>(t.dx) + h0 * t.dx_head + (int64_t)token * t.dx_token;
+    const int32_t* position_at = a.positions + (int64_t)token * a.table.axes + ch.axis;
+    const int64_t x_step = (int64_t)step * t.x_token, dy_step = (int64_t)step * t.dy_token, dx_step = (int64_t)step * t.dx_token;
+    auto fetch = [&](int stage) {
 #pragma unroll
         for (int i = 0; i < kGradHeadsPerChunk; ++i) {
-            const bool valid = of < a.n_tokens && i < rows;
-            ring.copy(stage, 2 * i, xs + of * t.x_token + i * t.x_head, valid);
-            ring.copy(stage, 2 * i + 1, dys + of * t.dy_token + i * t.dy_head, valid);
+            const bool valid = fetched < n_tokens && i < rows;
+            ring.copy(stage, 2 * i, x_at + i * t.x_head, valid);
+            ring.copy(stage, 2 * i + 1, dy_at + i * t.dy_head, valid);
         }
         ring.commit();
+        x_at += x_step, dy_at += dy_step, fetched += step;
     };
-    for (int i = 0; i < kStages - 1; ++i) fetch(i, token + i * step);
+    for (int i = 0; i < kStages - 1; ++i) fetch(i);
     float2 w[4], dw[4], db[4];
     load_channels(t.weight, ch, w, 1.f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) dw[i] = db[i] = make_float2(0.f, 0.f);
     int32_t position = 0;
-    if (token < a.n_tokens && ch.rotates) position = ld_global(a.positions + token * a.table.axes + ch.axis);
+    if (token < n_tokens && ch.rotates) position = ld_global(position_at);
     int stage = 0;
-    for (int64_t first = (int64_t)column * GROUPS; first < a.n_tokens; first += step, token += step) {
-        const bool here = token < a.n_tokens;
+    for (uint32_t first = (uint32_t)(column * GROUPS); first < n_tokens; first += step, token += step, dx_at += dx_step) {
+        const bool here = token < n_tokens;
         Turn cs;
         if (here && ch.rotates) cs = load_turn(a.table, ch, position, a.status);
-        if (token + step < a.n_tokens && ch.rotates) position = ld_global(a.positions + (token + step) * a.table.axes + ch.axis);
+        position_at += (int64_t)step * a.table.axes;
+        if (token + step < n_tokens && ch.rotates) position = ld_global(position_at);
         ring.arrived();
-        fetch(stage == 0 ? kStages - 1 : stage - 1, token + (kStages - 1) * step);
+        fetch(stage == 0 ? kStages - 1 : stage - 1);
 #pragma unroll
         for (int i = 0; i < kGradHeadsPerChunk; ++i) {
             const bool exists = here && i < rows;
@@ -339,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_grad_kernel(const __grid_con
                 for (int c = 0; c < 4; ++c) dw[c] = tc::ffma2(tc::fmul2(g[c], make_float2(r, r)), x[c], dw[c]), db[c] = tc::fadd2(db[c], g[c]);
             }
             if (exists) {
-                T* dx = dxs + i * t.dx_head + token * t.dx_token;
+                T* dx = dx_at + i * t.dx_head;
                 *reinterpret_cast<uint2*>(dx + ch.a) = pack4<T>(u);
                 *reinterpret_cast<uint2*>(dx + ch.b) = pack4<T>(u + 2);
             }
