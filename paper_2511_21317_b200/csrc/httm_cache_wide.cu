@@ -64,6 +64,14 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
         "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
         : "memory");
 }
+// Behind tmem_wait_ld: what has been loaded may be used from here on (the wait itself names no registers, so nothing else would keep uses behind it).
+template <int N>
+__device__ __forceinline__ void loaded(uint32_t (&v)[N]) {
+    static_assert(N % 8 == 0, "eight registers at a time");
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+        asm volatile("" : "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7]));
+}
 template <int NB>
 __device__ __forceinline__ uint32_t uses(int n, int r) {   // how many of 0 .. n - 1 are r modulo NB
     return (uint32_t)((n - r + NB - 1) / NB);
@@ -403,6 +411,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         tc::tmem_ld8(t_s + at, v);
                         tc::tmem_ld8(t_s + at + 8, v + 8);
                         tc::tmem_wait_ld();
+                        loaded(v);
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
                             if (at + i >= limit) v[i] = 0xff800000u;
@@ -418,6 +427,8 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     tc::tmem_ld32(t_s + at, v0);
                     tc::tmem_ld32(t_s + at + 32, v1);
                     tc::tmem_wait_ld();
+                    loaded(v0);
+                    loaded(v1);
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
                         top0 = max3_nan(top0, __uint_as_float(v0[i]), __uint_as_float(v0[i + 1]));
@@ -439,6 +450,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                             uint32_t o[8];
                             tc::tmem_ld8(t_o + cc, o);
                             tc::tmem_wait_ld();
+                            loaded(o);
 #pragma unroll
                             for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
                             tc::tmem_st8(t_o + cc, o);
@@ -466,14 +478,19 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                 };
                 tc::tmem_wait_ld();
+                loaded(v0);
 #pragma unroll
                 for (int at = 0; at < BN; at += 64) {   // (P covers columns whose scores have been read)
                     tc::tmem_ld32(t_s + at + 32, v1);
                     weights(v0, t_s + kPColumn + at / 2);
                     tc::tmem_wait_ld();
+                    loaded(v1);
                     if (at == 0) tc::tmem_ld32(t_s + 64, v0);
                     weights(v1, t_s + kPColumn + at / 2 + 16);
-                    tc::tmem_wait_ld();
+                    if (at == 0) {
+                        tc::tmem_wait_ld();
+                        loaded(v0);
+                    }
                 }
                 l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
                 tc::tmem_wait_st();
@@ -517,12 +534,14 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     uint32_t o[32];
                     tc::tmem_ld32(t_o + c, o);
                     tc::tmem_wait_ld();
+                    loaded(o);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fa);
                     if (!pair) {
                         uint32_t ob[32];
                         tc::tmem_ld32(t_o + D + c, ob);   // O_B lies behind O_A
                         tc::tmem_wait_ld();
+                        loaded(ob);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(fmaf(__uint_as_float(ob[i]), fb, __uint_as_float(o[i])));
                     }

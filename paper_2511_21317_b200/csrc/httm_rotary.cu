@@ -205,41 +205,44 @@ __global__ void __launch_bounds__(kThreads, 3) rows_kernel(const __grid_constant
     const int rows = min(kHeadsPerChunk, t.heads - h0);
     depend_wait();
     dependents_launch();
-    const T* in = static_cast<const T*>(t.in) + h0 * t.in_head + 8 * lane;
-    T* out = static_cast<T*>(t.out) + h0 * t.out_head;
-    const int64_t step = (int64_t)gridDim.x * GROUPS;
-    int64_t token = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
-    auto fetch = [&](int stage, int64_t of) {
+    // (token numbers stay below 2^31 plus a few grids; addresses are carried along, each turn adds one stride to them)
+    const uint32_t n_tokens = (uint32_t)a.n_tokens, step = gridDim.x * GROUPS;
+    uint32_t token = blockIdx.x * GROUPS + threadIdx.x / LANES, fetched = token;
+    const T* in = static_cast<const T*>(t.in) + h0 * t.in_head + 8 * lane + (int64_t)token * t.in_token;
+    T* out = static_cast<T*>(t.out) + h0 * t.out_head + (PAGED ? 0 : (int64_t)token * t.out_token);
+    const int32_t* position_at = a.positions + (int64_t)token * table.axes + ch.axis;
+    const int64_t in_step = (int64_t)step * t.in_token, out_step = PAGED ? 0 : (int64_t)step * t.out_token;
+    auto fetch = [&](int stage) {
 #pragma unroll
-        for (int i = 0; i < kHeadsPerChunk; ++i) ring.copy(stage, i, in + of * t.in_token + i * t.in_head, of < a.n_tokens && i < rows);
+        for (int i = 0; i < kHeadsPerChunk; ++i) ring.copy(stage, i, in + i * t.in_head, fetched < n_tokens && i < rows);
         ring.commit();
+        in += in_step, fetched += step;
     };
-    for (int i = 0; i < kStages - 1; ++i) fetch(i, token + i * step);
+    for (int i = 0; i < kStages - 1; ++i) fetch(i);
     float2 w[4], b[4];
     load_channels(t.weight, ch, w, 1.f);
     load_channels(t.bias, ch, b, -0.f);   // (x + -0 is x, a zero's sign included)
     // a token's position and place are read one turn ahead: the table's row is not another trip to memory behind them
     int32_t position = 0, slot = 0;
-    auto look_ahead = [&](int64_t next) {
-        if (next >= a.n_tokens) return;
-        if (ch.rotates) position = ld_global(a.positions + next * table.axes + ch.axis);
-        if (PAGED) slot = ld_global(a.slots + next);
+    auto look_ahead = [&](uint32_t next) {
+        if (next < n_tokens) {
+            if (ch.rotates) position = ld_global(position_at);
+            if (PAGED) slot = ld_global(a.slots + next);
+        }
+        position_at += (int64_t)step * table.axes;
     };
     look_ahead(token);
     // (all lanes of a warp go through the loop together: the sums over a row exchange between lanes)
     int stage = 0;
-    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < a.n_tokens; first += step, token += step) {
-        const bool here = token < a.n_tokens;
+    for (uint32_t first = blockIdx.x * GROUPS; first < n_tokens; first += step, token += step, out += out_step) {
+        const bool here = token < n_tokens;
         Turn cs;
         if (here && ch.rotates) cs = load_turn(table, ch, position, a.status);
         T* dst = out;
-        if (PAGED)
-            dst += (int64_t)(slot >> a.page_shift) * t.out_page + (int64_t)(slot & ((1 << a.page_shift) - 1)) * t.out_token;
-        else
-            dst += token * t.out_token;
+        if (PAGED) dst += (int64_t)(slot >> a.page_shift) * t.out_page + (int64_t)(slot & ((1 << a.page_shift) - 1)) * t.out_token;
         look_ahead(token + step);
         ring.arrived();
-        fetch(stage == 0 ? kStages - 1 : stage - 1, token + (kStages - 1) * step);
+        fetch(stage == 0 ? kStages - 1 : stage - 1);
 #pragma unroll
         for (int i = 0; i < kHeadsPerChunk; ++i) {
             float2 x[4];   // (a row that does not exist: whatever the stage holds, not stored)
