@@ -13,8 +13,8 @@
 // strides; rows that a tile does not fill compute something that nobody stores.  Keys behind the end of the prefix or of a sequence are masked
 // by -inf, and the values in their places are set to zero in shared memory, because pages hold anything there and 0 x NaN is not 0.
 //
-// A row's stabiliser is the largest score at the time it was set, and is raised only when a tile exceeds it by more than 2^8: weights of up to
-// 2^8 cost no precision (they are rounded relative to themselves, and sums are 32-bit), and raising it rewrites the accumulator.
+// A row's stabiliser is the largest score at the time it was set and stays as long as no weight overflows: weights above 1 cost no precision (they are
+// rounded relative to themselves, and sums are 32-bit), raising it rewrites the accumulator, and looking for it costs a pass over the scores.
 #include "httm_cache.cuh"
 #include "tc_exp2.cuh"
 #include "tc_sm100.cuh"
@@ -29,6 +29,7 @@ constexpr int kTmemColumns = 512;
 constexpr int kSubTile = BM * 128;   // 128 rows of 64 channels
 constexpr int kPColumn = 0;          // P (16-bit pairs, 64 columns) lies over the first 64 columns of its S
 constexpr float kRaise = 8.f;        // in units of log2
+constexpr float kSumLimit = 1.2676506e30f;   // 2^100
 // Of every eight pairs of scores, those whose bit is set here take the polynomial (FMA pipe), the others the special-function unit.
 constexpr uint32_t kPolyPairs = 0x11;
 
@@ -92,12 +93,72 @@ __device__ __forceinline__ KeyTile key_tile(const CacheSeg& seg, int tile) {
     return t;
 }
 
+// A tile whose weights overflowed, done again for the rows that this happened to (q_row: null for the others, whose weights stay): its scores are recomputed from global memory (the weights lie over half of them, the key tile
+// may have been replaced), first for their maximum, then for the weights 2^(s - m'), m' = max(m, max s).  Returns m' and the row's sum of weights.
+// Only scores that rise by more than 69 (100 in units of log2) from one key tile to another come here: it need not be fast, only right, and out of line
+// it costs the ordinary tiles nothing.
+template <typename T, int D>
+__device__ __noinline__ float2 redo_tile(const CacheArgs& a, const void* q_row, int head, int table, int key0, int limit, float m, uint32_t t_p) {
+    auto values = [](int4 u, float* v) {
+        const uint32_t w[4] = {(uint32_t)u.x, (uint32_t)u.y, (uint32_t)u.z, (uint32_t)u.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float2 f;
+            if constexpr (std::is_same<T, __half>::value)
+                f = __half22float2(*reinterpret_cast<const __half2*>(&w[e]));
+            else
+                f = make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+            v[2 * e] = f.x, v[2 * e + 1] = f.y;
+        }
+    };
+    auto score = [&](int i) {
+        if (!q_row || i >= limit) return -INFINITY;
+        const int key = key0 + i;
+        const int64_t page = ld_l2(a.table + table + (key >> a.page_shift));
+        const T* k = static_cast<const T*>(a.k) + head * a.k_head + page * a.k_page + (key & ((1 << a.page_shift) - 1)) * a.k_slot;
+        float sum = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 8) {
+            float x[8], y[8];
+            values(ld_l2_16(static_cast<const T*>(q_row) + c), x);
+            values(ld_l2_16(k + c), y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], y[e], sum);
+        }
+        return sum * a.scale_log2;
+    };
+    float top = m;
+#pragma unroll 1
+    for (int i = 0; i < BN; ++i) top = fmaxf(top, score(i));
+    const float from = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll 1
+    for (int at = 0; at < BN; at += 16) {
+        uint32_t pk[8];
+        __syncwarp();
+        tc::tmem_ld8(t_p + at / 2, pk);
+        tc::tmem_wait_ld();
+        loaded(pk);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float e0 = exp2f(score(at + 2 * i) - from), e1 = exp2f(score(at + 2 * i + 1) - from);
+            sum += e0 + e1;
+            if (q_row) pk[i] = pack2<T>(e0, e1);
+        }
+        __syncwarp();
+        tc::tmem_st8(t_p + at / 2, pk);
+    }
+    return make_float2(top, sum);
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
 cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ CacheArgs a) {
     using S = Shape<D>;
     constexpr int NB = S::NB, SUB = S::SUB, TILE = S::TILE;
+    constexpr bool kHalf = std::is_same<T, __half>::value;
+    constexpr int kMaxUnroll = kHalf ? 2 : 1;   // (where it is done once a job it need not be fast, but small)
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t s_q = tc::smem_addr(smem), s_k = s_q + 2 * TILE, s_v = s_k + NB * TILE;
@@ -228,7 +289,6 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     } else if (warp == 1) {
         // ------------------------------------------------------------------ products
         if (tc::elect_one()) {
-            constexpr bool kHalf = std::is_same<T, __half>::value;
             constexpr uint32_t kTypes = (1u << 7) | (1u << 10);   // A and B are bf16; without these bits fp16
             // a negative scale turns the sign of Q in the product (bit 13), so that the largest product is the largest score
             const uint32_t idesc_qk = (tc::idesc_bf16(BM, BN, false, false) & ~(kHalf ? kTypes : 0u)) | (a.scale_log2 < 0.f ? 1u << 13 : 0u);
@@ -364,7 +424,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         int jobs = 0;
         for (int jb = job_first; ok && jb < job_last; ++jb, ++jobs) {
             // (few registers are left beside the scores: what only the job's end needs is read again there)
-            int n_score, n_own, tile0, n_prefix, prefix_keys, seen_to;
+            int n_score, n_own, tile0, n_prefix, prefix_keys, seen_to, tokens;
             bool pair;
             {
                 const CacheJob job = ld_record(a.jobs + jb);
@@ -377,8 +437,9 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 tile0 = job.tile0;
                 prefix_keys = seg.prefix_keys;
                 n_prefix = (prefix_keys + BN - 1) / BN;
-                // own keys that the row sees, counted like the tiles: behind the prefix's last, which is filled up
-                seen_to = n_prefix * BN + (token < seg.tokens ? min(seg.own_keys, seg.seen0 + token * seg.seen_step) : 0);
+                tokens = seg.tokens;
+                // own keys that the row sees, counted like the tiles: behind the prefix's last, which is filled up (a row that does not exist sees all of them)
+                seen_to = n_prefix * BN + (token < seg.tokens ? min(seg.own_keys, seg.seen0 + token * seg.seen_step) : seg.own_keys);
             }
             float m = -INFINITY, l = 0.f;
             {   // the accumulator starts at zero: every P V adds to it (ordered before the first arrival at p_full)
@@ -389,6 +450,23 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 for (int c = 0; c < D; c += 32) tc::tmem_st32(t_o + c, z);
                 if (n_own == 0) tc::tmem_wait_st();
             }
+            const bool exists = row / a.group < tokens;
+            // The accumulator times f, once the group's last P V is done (the next is issued behind the P of the tile at hand).
+            auto rescale = [&](float f, uint32_t j) {
+                if (!__all_sync(0xffffffffu, tc::mbar_wait(bar(bars->o_done[x]), (od_base + j - 1) & 1u, abort_flag))) return false;
+                tc::fence_after_sync();
+#pragma unroll 1
+                for (int cc = 0; cc < D; cc += 8) {
+                    uint32_t o[8];
+                    tc::tmem_ld8(t_o + cc, o);
+                    tc::tmem_wait_ld();
+                    loaded(o);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                    tc::tmem_st8(t_o + cc, o);
+                }
+                return true;
+            };
             int buf = x, round = 0;   // score tile 2 j + x is in buffer `buf`, used for the `round`-th time in this job
             for (int j = 0; j < n_own; ++j) {
                 const uint32_t t_s = tmem + buf * BN + lane_addr;
@@ -421,45 +499,38 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     tc::tmem_wait_st();
                 }
                 uint32_t v0[32], v1[32];
-                float top0 = -INFINITY, top1 = -INFINITY;   // not a number if one of the scores is not
+                // bf16: the stabiliser is the maximum of the first tile in which the row sees a key; later tiles go without a pass for theirs and are done again if
+                // their weights overflow (a sum of 2^100: weights, sums and accumulators do not care about a common factor below that).
+                // fp16, whose weights end at 2^16: every tile's maximum, and the stabiliser is raised where it exceeds it by more than 2^8.
+                const bool look = kHalf || __any_sync(0xffffffffu, m == -INFINITY);
+                if (look) {
+                    float top0 = -INFINITY, top1 = -INFINITY;   // not a number if one of the scores is not
+#pragma unroll kMaxUnroll
+                    for (int at = 0; at < BN; at += 64) {
+                        tc::tmem_ld32(t_s + at, v0);
+                        tc::tmem_ld32(t_s + at + 32, v1);
+                        tc::tmem_wait_ld();
+                        loaded(v0);
+                        loaded(v1);
 #pragma unroll
-                for (int at = 0; at < BN; at += 64) {
-                    tc::tmem_ld32(t_s + at, v0);
-                    tc::tmem_ld32(t_s + at + 32, v1);
-                    tc::tmem_wait_ld();
-                    loaded(v0);
-                    loaded(v1);
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        top0 = max3_nan(top0, __uint_as_float(v0[i]), __uint_as_float(v0[i + 1]));
-                        top1 = max3_nan(top1, __uint_as_float(v1[i]), __uint_as_float(v1[i + 1]));
+                        for (int i = 0; i < 32; i += 2) {
+                            top0 = max3_nan(top0, __uint_as_float(v0[i]), __uint_as_float(v0[i + 1]));
+                            top1 = max3_nan(top1, __uint_as_float(v1[i]), __uint_as_float(v1[i + 1]));
+                        }
+                    }
+                    const float top = max3_nan(top0, top1, -INFINITY) * c;
+                    const bool raise = kHalf ? !(top <= m + kRaise) : m == -INFINITY;   // (also where top is not a number)
+                    if (__any_sync(0xffffffffu, raise)) {
+                        const float f = raise ? exp2f(m - top) : 1.f;
+                        if (raise && !(top == -INFINITY)) m = top, l *= f;
+                        if (kHalf && j > 0 && !(ok = rescale(raise ? f : 1.f, (uint32_t)j))) break;
                     }
                 }
                 tc::tmem_ld32(t_s, v0);
-                const float top = max3_nan(top0, top1, -INFINITY) * c;
-                const bool raise = !(top <= m + kRaise);   // (also where top is not a number)
-                if (__any_sync(0xffffffffu, raise)) {
-                    const float f = raise ? exp2f(m - top) : 1.f;
-                    if (raise) m = top;
-                    l *= f;
-                    if (j > 0) {   // the accumulator is at rest once the group's last P V is done; the next is issued behind this tile's P
-                        if (!(ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->o_done[x]), (od_base + (uint32_t)(j - 1)) & 1u, abort_flag)))) break;
-                        tc::fence_after_sync();
-#pragma unroll 1
-                        for (int cc = 0; cc < D; cc += 8) {
-                            uint32_t o[8];
-                            tc::tmem_ld8(t_o + cc, o);
-                            tc::tmem_wait_ld();
-                            loaded(o);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tc::tmem_st8(t_o + cc, o);
-                        }
-                    }
-                }
                 const float from = m == -INFINITY ? 0.f : m;
                 const float2 c2 = make_float2(c, c), neg = make_float2(-from, -from);
                 float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+                float odd = -INFINITY;   // the polynomial makes a number of what is none: seen here
                 auto weights = [&](const uint32_t (&v)[32], uint32_t to) {   // 32 scores -> 16 columns of P
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
@@ -468,6 +539,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         for (int i = 0; i < 8; ++i) {
                             const float2 u = tc::ffma2(make_float2(__uint_as_float(v[g * 16 + 2 * i]), __uint_as_float(v[g * 16 + 2 * i + 1])), c2, neg);
                             const float2 e = (kPolyPairs >> i) & 1u ? exp2_poly2(u) : make_float2(fast_exp2(u.x), fast_exp2(u.y));
+                            if (!kHalf && ((kPolyPairs >> i) & 1u)) odd = max3_nan(odd, u.x, u.y);
                             if (i & 1)
                                 sum1 = tc::fadd2(sum1, e);
                             else
@@ -492,7 +564,28 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         loaded(v0);
                     }
                 }
-                l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+                float tile_sum = (sum0.x + sum0.y) + (sum1.x + sum1.y);
+                if (!kHalf && odd != odd) tile_sum = odd;
+                if (!kHalf && __any_sync(0xffffffffu, exists && tile_sum >= kSumLimit)) {   // (a sum that is not a number stays one)
+                    const bool mine = exists && tile_sum >= kSumLimit;
+                    const CacheJob job = ld_record(a.jobs + jb);
+                    const CacheSeg seg = ld_record(a.segs + job.seg + (pair ? x : 0));
+                    const int token = mine ? row / a.group : 0, gi = mine ? row % a.group : 0;
+                    const T* q_row = static_cast<const T*>(a.q) + (int64_t)(seg.token0 + token) * a.q_token + (int64_t)(job.head * a.group + gi) * a.q_head;
+                    const bool own = tile >= n_prefix;
+                    tc::tmem_wait_st();
+                    const float2 again = redo_tile<T, D>(a, mine ? q_row : nullptr, job.head, own ? seg.own_table : 0, (own ? tile - n_prefix : tile) * BN,
+                                                         min(limit, BN), m, t_s + kPColumn);
+                    float f = 1.f;
+                    if (mine) {
+                        f = exp2f(m - again.x);
+                        m = again.x;
+                        l *= f;
+                        tile_sum = again.y;
+                    }
+                    if (j > 0 && !(ok = rescale(f, (uint32_t)j))) break;
+                }
+                l += tile_sum;
                 tc::tmem_wait_st();
                 tc::fence_before_sync();
                 tc::mbar_arrive(p_full);

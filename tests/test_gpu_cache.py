@@ -194,6 +194,24 @@ def test_an_infinite_score_below_all_others():
     assert not got.isnan().any() and not torch.equal(got, ref)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_one_key_that_is_not_a_number_reaches_every_row_that_sees_it(dtype):
+    """Whatever the place of the key in its tile, and whether it is the row's first tile or not."""
+    sc = Scene([300, 10], [290, 1], 200, 4, 2, 64, 16, dtype=dtype, seed=11)
+    ref = sc.cache.attention(sc.batch, sc.q).clone()
+    for place in list(range(16)) + [130, 137, 199]:
+        p, slot = sc.prefix_pages[place // 16], place % 16
+        kept = sc.pools[0][p, :, slot].clone()
+        sc.pools[0][p, :, slot, 3] = float("nan")
+        assert sc.cache.attention(sc.batch, sc.q).isnan().all(), place
+        sc.pools[0][p, :, slot] = kept
+    p = sc.tables[0][100 // 16]   # an own key that tokens 90 .. of the first sequence see (token i sees keys up to 10 + i)
+    for slot in range(100 % 16, 100 % 16 + 1):
+        sc.pools[0][p, :, slot, 3] = float("nan")
+        got = sc.cache.attention(sc.batch, sc.q)
+        assert got[90:290].isnan().all() and torch.equal(got[:90], ref[:90]) and torch.equal(got[290:], ref[290:])
+
+
 def test_append_then_attend():
     """Tokens go to their places and nothing else is written; the attention then sees them."""
     for dtype, dim, page, order, layout in ((torch.bfloat16, 64, 16, "nhsd", "fused"), (torch.float16, 128, 64, "nshd", "heads"),
