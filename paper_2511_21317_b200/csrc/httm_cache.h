@@ -115,11 +115,11 @@ struct alignas(16) CacheJob {   // key tiles [tile0, tile1) of a row tile: those
     int32_t part2;              // of the second row tile
     int32_t pad;
 };
-constexpr int kCombineWarps = 8, kCombineRows = 8;
+constexpr int kCombineWarps = 8, kCombineRows = 8, kCombineFewRows = 2, kCombineManyParts = 16;
 struct alignas(16) CombineTask {   // rows of one key head whose partial results are to be added up
     int32_t token0, first_head;    // the first row: token, head of the group; the others follow, the group's heads of a token side by side
-    int32_t rows;                  // at most kCombineRows
-    int32_t head;
+    int32_t rows, room;            // at most `room`: kCombineRows, or kCombineFewRows where a few rows have more than kCombineManyParts parts
+    int32_t head, pad[3];
     // of the row tile that looks at the prefix, and of the one that looks at the own keys: first unit and number of the partial results, rows of the tile,
     // this task's first row in it (0 parts: there is no such tile)
     int32_t unit[2], parts[2], tile_rows[2], row[2];

@@ -334,18 +334,14 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) cache_narrow_kernel
 
 // The partial results of rows whose keys were shared out, added up in the order of the keys: out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m).  A part of a tile
 // of R rows is [D / 4][R] quads of channels and then [R] pairs (m, l): the thread of a row in the wide kernel writes with its neighbours whole lines (row
-// by row they were 32 half sectors per instruction, 4 600 .. 7 000 ns at the end of a job).  A CTA takes eight rows; its warps take the parts in turn, a lane
-// the quads q, q + 4, .. of one row, and the warps' sums meet in shared memory.  The time is that of trips to L2 behind one another, so values
+// by row they were 32 half sectors per instruction, 4 600 .. 7 000 ns at the end of a job).  A CTA takes eight rows, or two (a whole sector) that have many parts; its warps take the parts in
+// turn, a lane some of the quads of one row, and the warps' sums meet in shared memory.  The time is that of trips to L2 behind one another, so values
 // are asked for together with the maxima that weight them.  A row without parts gets zeros.
-template <typename T, int D>
-__global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const __grid_constant__ CacheArgs a) {
-    constexpr int Q = D / 16, BATCH = 8 / Q * 2;   // quads of a lane; parts that it asks for at a time (4, or 2 for 128 channels)
-    __shared__ __align__(16) float sums[kCombineWarps][kCombineRows][D + 4];
-    __shared__ float2 stats[kCombineWarps][kCombineRows];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane & 7, quad = lane >> 3;
-    const CombineTask task = ld_record(a.combine_tasks + blockIdx.x);
-    depend_wait();
-    dependents_launch();
+template <typename T, int D, int ROWS>
+__device__ __forceinline__ void combine_rows(const CacheArgs& a, const CombineTask& task, float (*sums)[kCombineRows][D + 4], float2 (*stats)[kCombineRows]) {
+    constexpr int STEP = 32 / ROWS, Q = D / 4 / STEP;   // a lane has the quads q, q + STEP, ..: Q of them
+    constexpr int BATCH = Q < 2 ? 8 : 16 / Q;           // parts that it asks for at a time
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane % ROWS, quad = lane / ROWS;
     const int n0 = task.parts[0], n = n0 + task.parts[1];   // those of the prefix come first
     const float* base[2];
     int64_t stride[2];
@@ -373,7 +369,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const
                     const float* part = base[k] + (p - (k ? n0 : 0)) * stride[k];
                     st[i] = __ldcg(reinterpret_cast<const float2*>(part + tile_rows * D) + at);
 #pragma unroll
-                    for (int c = 0; c < Q; ++c) v[i][c] = __ldcg(reinterpret_cast<const float4*>(part) + (quad + 4 * c) * tile_rows + at);
+                    for (int c = 0; c < Q; ++c) v[i][c] = __ldcg(reinterpret_cast<const float4*>(part) + (quad + STEP * c) * tile_rows + at);
                 }
             }
             float high = top;
@@ -396,7 +392,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const
         }
         if (warp < n) {
 #pragma unroll
-            for (int c = 0; c < Q; ++c) *reinterpret_cast<float4*>(&sums[warp][row][4 * (quad + 4 * c)]) = sum[c];
+            for (int c = 0; c < Q; ++c) *reinterpret_cast<float4*>(&sums[warp][row][4 * (quad + STEP * c)]) = sum[c];
             if (quad == 0) stats[warp][row] = make_float2(top, total);
         }
     }
@@ -419,6 +415,19 @@ __global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const
         T* out = static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + 4 * c;
         *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
     }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const __grid_constant__ CacheArgs a) {
+    __shared__ __align__(16) float sums[kCombineWarps][kCombineRows][D + 4];
+    __shared__ float2 stats[kCombineWarps][kCombineRows];
+    const CombineTask task = ld_record(a.combine_tasks + blockIdx.x);
+    depend_wait();
+    dependents_launch();
+    if (task.room == kCombineRows)
+        combine_rows<T, D, kCombineRows>(a, task, sums, stats);
+    else
+        combine_rows<T, D, kCombineFewRows>(a, task, sums, stats);
 }
 
 template <typename F>

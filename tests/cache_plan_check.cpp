@@ -145,7 +145,7 @@ static bool one_round() {
     // rows that are written by a job, and rows whose partial results are added up: every row exactly once
     std::vector<int> written((size_t)tokens * c.heads, 0);   // (token, query head)
     for (const CombineTask& k : p.combine_tasks) {
-        NEED(k.rows > 0 && k.rows <= kCombineRows);
+        NEED(k.rows > 0 && k.rows <= k.room && (k.room == kCombineRows || k.room == kCombineFewRows));
         NEED(k.first_head >= 0 && k.first_head < group && k.head >= 0 && k.head < c.kv_heads && k.token0 >= 0);
         for (int r = 0; r < k.rows; ++r) {
             const int i = k.token0 + (k.first_head + r) / group, g = (k.first_head + r) % group;
