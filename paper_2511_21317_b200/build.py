@@ -1,4 +1,4 @@
-"""Build libhttm.so (CUDA, sm_100a) in-tree with nvcc.
+"""Build libhttm.so (CUDA, sm_100a) in-tree with nvcc, and the module that calls it on torch tensors with g++.
 
     python -m paper_2511_21317_b200.build [--force] [--verbose]
 
@@ -11,12 +11,14 @@ import os
 import re
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libhttm.so")
+CALLS = os.path.join(HERE, "_kv_cache_calls.so")   # Python module: csrc/kv_cache_calls.cpp
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["httm_api.cu", "httm_small_blocks.cu", "httm_mid_blocks.cu", "httm_mem_kernels.cu", "httm_attention_tc.cu", "httm_big_blocks.cu", "httm_linear.cu", "httm_static.cu",
            "httm_umma_selftest.cu", "httm_rotary.cu", "httm_batch.cu", "httm_cache_narrow.cu", "httm_cache_wide.cu"]
@@ -48,7 +50,28 @@ def _deps_mtime() -> float:
     return max(os.path.getmtime(p) for p in paths)
 
 
+def build_calls(force: bool = False) -> str:
+    """The Python module that checks torch tensors and calls the library (host code; needs torch's headers)."""
+    src = os.path.join(CSRC, "kv_cache_calls.cpp")
+    newest = max(os.path.getmtime(p) for p in (src, os.path.join(INCLUDE, "httm.h"), __file__))
+    if not force and os.path.exists(CALLS) and os.path.getmtime(CALLS) >= newest:
+        return CALLS
+    import torch
+    root = os.path.dirname(torch.__file__)
+    tmp = CALLS + f".{os.getpid()}.tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-I", INCLUDE, "-isystem", os.path.join(root, "include"),
+           "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
+           "-isystem", "/usr/local/cuda/include", src, "-o", tmp, "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_python", "-ltorch_cpu", "-ltorch"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+        raise RuntimeError("g++ failed on kv_cache_calls.cpp")
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_calls(force)
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _deps_mtime():
         return LIB
     os.makedirs(OBJ_DIR, exist_ok=True)

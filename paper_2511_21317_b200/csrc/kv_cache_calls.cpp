@@ -1,0 +1,286 @@
+// The calls of the operators around a kept scene from Python: checks of the tensors, marshalling, and the call of the C ABI, in one step.
+//
+// A call on a few tokens takes the GPU 2 - 7 us; attribute by attribute in Python its nine tensors cost more than that (host time of norm_rotate
+// on one token with ctypes 11.4 us, with this 4.9; of its gradients 24 and 10.4, of append 9.4 and 5.1, of an attention of two kernels 12.8 and 8.3).  The functions get a handle, the sizes that the Python object keeps, and tensors or None; they raise
+// HttmError with the library's codes.  Nothing is kept from call to call.
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+
+#include <ATen/ATen.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <string>
+
+#include "httm.h"
+
+namespace {
+
+struct Abi {
+    decltype(&httm_norm_rotate) norm_rotate = nullptr;
+    decltype(&httm_norm_rotate_backward) norm_rotate_backward = nullptr;
+    decltype(&httm_cache_append) append = nullptr;
+    decltype(&httm_cache_attention) attention = nullptr;
+    decltype(&httm_last_error) last_error = nullptr;
+} g_abi;
+PyObject* g_error = nullptr;   // HttmError
+
+struct Failure {   // becomes an HttmError
+    int code;
+    std::string message;
+};
+[[noreturn]] void bad(const std::string& message) { throw Failure{HTTM_ERR_INVALID_ARG, message}; }
+void check(int rc) {
+    if (rc != HTTM_OK) throw Failure{rc, g_abi.last_error(nullptr)};
+}
+
+int64_t integer(PyObject* o) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        bad("an argument is not a whole number");
+    }
+    return v;
+}
+template <typename H>
+H* handle(PyObject* o) {
+    if (o == Py_None) bad("the handle is closed");
+    return reinterpret_cast<H*>(integer(o));
+}
+const at::Tensor* tensor(PyObject* o, const char* name) {   // null for None
+    if (o == Py_None) return nullptr;
+    if (!THPVariable_Check(o)) bad(std::string(name) + ": expected a tensor");
+    return &THPVariable_Unpack(o);
+}
+std::string where(int64_t device) { return " on cuda:" + std::to_string(device); }
+
+int32_t kind_of(at::ScalarType t, const char* name) {
+    if (t == at::kBFloat16) return HTTM_BF16;
+    if (t == at::kHalf) return HTTM_FP16;
+    bad(std::string(name) + ": expected bfloat16 or float16");
+}
+bool lives(const at::Tensor& t, at::ScalarType dtype, int64_t device) { return t.scalar_type() == dtype && t.is_cuda() && t.get_device() == device; }
+httm_tensor rows(const at::Tensor& t, const char* name, int64_t heads, int64_t tokens, int64_t dim, at::ScalarType dtype, int64_t device) {
+    if (!lives(t, dtype, device)) bad(std::string(name) + ": expected a " + c10::toString(dtype) + " tensor" + where(device));
+    if (t.dim() != 3 || t.size(0) != heads || t.size(1) != tokens || t.size(2) != dim)
+        bad(std::string(name) + ": expected shape [" + std::to_string(heads) + " heads][" + std::to_string(tokens) + " tokens][" + std::to_string(dim) + "]");
+    if (t.stride(2) != 1) bad(std::string(name) + ": channels must be contiguous");
+    return httm_tensor{t.data_ptr(), t.stride(0), t.stride(1)};
+}
+float* vec(const at::Tensor* t, const char* name, int64_t dim, int64_t device) {
+    if (!t) return nullptr;
+    if (!lives(*t, at::kFloat, device) || t->dim() != 1 || t->size(0) != dim || !t->is_contiguous())
+        bad(std::string(name) + ": expected a contiguous float32 vector of head_dim = " + std::to_string(dim) + where(device));
+    return static_cast<float*>(t->data_ptr());
+}
+const int32_t* positions_of(const at::Tensor* t, int64_t tokens, int64_t axes, int64_t device) {
+    if (!t) return nullptr;
+    const bool shape = (t->dim() == 2 && t->size(0) == tokens && t->size(1) == axes) || (t->dim() == 1 && axes == 1 && t->size(0) == tokens);
+    if (!lives(*t, at::kInt, device) || !shape || !t->is_contiguous())
+        bad("positions: expected a contiguous int32 tensor [" + std::to_string(tokens) + "][" + std::to_string(axes) + "]" + where(device));
+    return static_cast<const int32_t*>(t->data_ptr());
+}
+void* stream_of(PyObject* o, int64_t device) {   // an address, or None: the current stream
+    if (o != Py_None) return reinterpret_cast<void*>(integer(o));
+    return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
+}
+PyObject* wrap(const at::Tensor* t, PyObject* given) {   // the tensor that was given, or a new one; None
+    if (given && given != Py_None) return Py_NewRef(given);
+    return t ? THPVariable_Wrap(*t) : Py_NewRef(Py_None);
+}
+
+template <typename F>
+PyObject* guarded(F f) {
+    try {
+        return f();
+    } catch (const Failure& e) {
+        PyObject* x = PyObject_CallFunction(g_error, "is", e.code, e.message.c_str());
+        if (x) {
+            PyErr_SetObject(g_error, x);
+            Py_DECREF(x);
+        }
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    }
+    return nullptr;
+}
+bool count(Py_ssize_t n, Py_ssize_t want) {
+    if (n != want) PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, n);
+    return n == want;
+}
+
+// bind(addresses of httm_norm_rotate, httm_norm_rotate_backward, httm_cache_append, httm_cache_attention, httm_last_error; HttmError)
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count(n, 6)) return nullptr;
+    void* at[5];
+    for (int i = 0; i < 5; ++i) {
+        at[i] = PyLong_AsVoidPtr(a[i]);
+        if (!at[i]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "null address");
+    }
+    g_abi.norm_rotate = reinterpret_cast<decltype(g_abi.norm_rotate)>(at[0]);
+    g_abi.norm_rotate_backward = reinterpret_cast<decltype(g_abi.norm_rotate_backward)>(at[1]);
+    g_abi.append = reinterpret_cast<decltype(g_abi.append)>(at[2]);
+    g_abi.attention = reinterpret_cast<decltype(g_abi.attention)>(at[3]);
+    g_abi.last_error = reinterpret_cast<decltype(g_abi.last_error)>(at[4]);
+    Py_XSETREF(g_error, Py_NewRef(a[5]));
+    Py_RETURN_NONE;
+}
+
+struct First {   // the tensor that says how many tokens of which type there are
+    int64_t tokens;
+    at::ScalarType dtype;
+    int32_t kind;
+};
+First first_of(const at::Tensor* q, const at::Tensor* k) {
+    const at::Tensor* t = q ? q : k;
+    if (!t) bad("neither q nor k");
+    if (t->dim() != 3) bad("expected [heads][tokens][head_dim]");
+    return First{t->size(1), t->scalar_type(), kind_of(t->scalar_type(), q ? "q" : "k")};
+}
+
+// norm_rotate(handle, head_dim, axes, rotated_dim, device, q, k, positions, q_weight, k_weight, q_bias, k_bias, out_q, out_k, stream) -> (out_q, out_k)
+PyObject* norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count(n, 15)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        httm_rotary* h = handle<httm_rotary>(a[0]);
+        const int64_t dim = integer(a[1]), axes = integer(a[2]), rotated = integer(a[3]), device = integer(a[4]);
+        const at::Tensor* x[2] = {tensor(a[5], "q"), tensor(a[6], "k")};
+        const First f = first_of(x[0], x[1]);
+        static const char* names[2][4] = {{"q", "out_q", "q_weight", "q_bias"}, {"k", "out_k", "k_weight", "k_bias"}};
+        httm_rows r[2];
+        at::Tensor made[2];
+        for (int i = 0; i < 2; ++i) {
+            if (!x[i]) continue;
+            const int64_t heads = x[i]->dim() == 3 ? x[i]->size(0) : -1;
+            r[i].x = rows(*x[i], names[i][0], heads, f.tokens, dim, f.dtype, device);
+            const at::Tensor* out = tensor(a[12 + i], names[i][1]);
+            if (!out) {
+                made[i] = at::empty({heads, f.tokens, dim}, x[i]->options());
+                out = &made[i];
+            }
+            r[i].y = rows(*out, names[i][1], heads, f.tokens, dim, f.dtype, device);
+            r[i].heads = (int32_t)heads;
+            r[i].weight = vec(tensor(a[8 + i], names[i][2]), names[i][2], dim, device);
+            r[i].bias = vec(tensor(a[10 + i], names[i][3]), names[i][3], dim, device);
+        }
+        const at::Tensor* p = rotated > 0 ? tensor(a[7], "positions") : nullptr;
+        if (rotated > 0 && !p) bad("positions are missing");
+        check(g_abi.norm_rotate(h, f.kind, f.tokens, positions_of(p, f.tokens, axes, device), x[0] ? &r[0] : nullptr, x[1] ? &r[1] : nullptr,
+                                stream_of(a[14], device)));
+        PyObject* out = PyTuple_New(2);
+        for (int i = 0; out && i < 2; ++i) PyTuple_SET_ITEM(out, i, x[i] ? wrap(&made[i], a[12 + i]) : Py_NewRef(Py_None));
+        return out;
+    });
+}
+
+// norm_rotate_backward(handle, head_dim, axes, rotated_dim, device, dq, dk, q, k, positions, q_weight, k_weight, q_bias, k_bias, out_q, out_k, stream)
+//   -> (dq, dk, dq_weight, dq_bias, dk_weight, dk_bias)
+PyObject* norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count(n, 17)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        httm_rotary* h = handle<httm_rotary>(a[0]);
+        const int64_t dim = integer(a[1]), axes = integer(a[2]), rotated = integer(a[3]), device = integer(a[4]);
+        const at::Tensor *dy[2] = {tensor(a[5], "dq"), tensor(a[6], "dk")}, *x[2] = {tensor(a[7], "q"), tensor(a[8], "k")};
+        const First f = first_of(x[0], x[1]);
+        static const char* names[2][5] = {{"q", "dq", "out_q", "q_weight", "q_bias"}, {"k", "dk", "out_k", "k_weight", "k_bias"}};
+        httm_rows_grad r[2];
+        at::Tensor made[2], sums[2][2];
+        for (int i = 0; i < 2; ++i) {
+            if (!x[i]) continue;
+            if (!dy[i]) bad(std::string(names[i][1]) + " is missing");
+            const int64_t heads = x[i]->dim() == 3 ? x[i]->size(0) : -1;
+            r[i].x = rows(*x[i], names[i][0], heads, f.tokens, dim, f.dtype, device);
+            r[i].dy = rows(*dy[i], names[i][1], heads, f.tokens, dim, f.dtype, device);
+            const at::Tensor* out = tensor(a[14 + i], names[i][2]);
+            if (!out) {
+                made[i] = at::empty({heads, f.tokens, dim}, x[i]->options());
+                out = &made[i];
+            }
+            r[i].dx = rows(*out, names[i][2], heads, f.tokens, dim, f.dtype, device);
+            r[i].heads = (int32_t)heads;
+            const at::Tensor *w = tensor(a[10 + i], names[i][3]), *b = tensor(a[12 + i], names[i][4]);
+            r[i].weight = vec(w, names[i][3], dim, device);
+            vec(b, names[i][4], dim, device);
+            if (w) sums[i][0] = at::empty({dim}, w->options());
+            if (b) sums[i][1] = at::empty({dim}, b->options());
+            r[i].dweight = w ? static_cast<float*>(sums[i][0].data_ptr()) : nullptr;
+            r[i].dbias = b ? static_cast<float*>(sums[i][1].data_ptr()) : nullptr;
+        }
+        const at::Tensor* p = rotated > 0 ? tensor(a[9], "positions") : nullptr;
+        if (rotated > 0 && !p) bad("positions are missing");
+        check(g_abi.norm_rotate_backward(h, f.kind, f.tokens, positions_of(p, f.tokens, axes, device), x[0] ? &r[0] : nullptr, x[1] ? &r[1] : nullptr,
+                                         stream_of(a[16], device)));
+        PyObject* out = PyTuple_New(6);
+        for (int i = 0; out && i < 2; ++i) {
+            PyTuple_SET_ITEM(out, i, x[i] ? wrap(&made[i], a[14 + i]) : Py_NewRef(Py_None));
+            for (int j = 0; j < 2; ++j) PyTuple_SET_ITEM(out, 2 + 2 * i + j, wrap(sums[i][j].defined() ? &sums[i][j] : nullptr, nullptr));
+        }
+        return out;
+    });
+}
+
+at::ScalarType type_of(int64_t kind) { return kind == HTTM_BF16 ? at::kBFloat16 : at::kHalf; }
+
+// append(batch, kv_heads, tokens, head_dim, device, kind, address of the two httm_pages, k, v, rotary, axes, positions, k_weight, k_bias, stream)
+PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count(n, 15)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        httm_batch* b = handle<httm_batch>(a[0]);
+        const int64_t heads = integer(a[1]), tokens = integer(a[2]), dim = integer(a[3]), device = integer(a[4]), kind = integer(a[5]);
+        const httm_pages* pages = reinterpret_cast<const httm_pages*>(integer(a[6]));
+        const at::Tensor *k = tensor(a[7], "k"), *v = tensor(a[8], "v");
+        if (!k || !v) bad("k or v is missing");
+        const httm_tensor tk = rows(*k, "k", heads, tokens, dim, type_of(kind), device), tv = rows(*v, "v", heads, tokens, dim, type_of(kind), device);
+        httm_rotary* r = a[9] == Py_None ? nullptr : handle<httm_rotary>(a[9]);
+        const at::Tensor* p = tensor(a[11], "positions");
+        if (p && !r) bad("positions without a rotary handle");
+        check(g_abi.append(b, (int32_t)kind, pages[0], pages[1], tk, tv, r, positions_of(p, tokens, integer(a[10]), device),
+                           vec(tensor(a[12], "k_weight"), "k_weight", dim, device), vec(tensor(a[13], "k_bias"), "k_bias", dim, device), stream_of(a[14], device)));
+        Py_RETURN_NONE;
+    });
+}
+
+// attention(batch, heads, tokens, head_dim, device, kind, address of the two httm_pages, q, out, scale, stream) -> out
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!count(n, 11)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        httm_batch* b = handle<httm_batch>(a[0]);
+        const int64_t heads = integer(a[1]), tokens = integer(a[2]), dim = integer(a[3]), device = integer(a[4]), kind = integer(a[5]);
+        const httm_pages* pages = reinterpret_cast<const httm_pages*>(integer(a[6]));
+        const at::Tensor *q = tensor(a[7], "q"), *out = tensor(a[8], "out");
+        if (!q) bad("q is missing");
+        const httm_tensor tq = rows(*q, "q", heads, tokens, dim, type_of(kind), device);
+        at::Tensor made;
+        if (!out) {
+            made = at::empty({tokens, heads * dim}, q->options());
+            out = &made;
+        }
+        if (!lives(*out, type_of(kind), device)) bad("out: expected a CUDA tensor of q's type");
+        httm_tensor to{out->data_ptr(), dim, 0};
+        if (out->dim() == 2 && out->size(0) == tokens && out->size(1) == heads * dim && out->stride(1) == 1)
+            to.stride_token = out->stride(0);
+        else if (out->dim() == 3 && out->size(0) == tokens && out->size(1) == heads && out->size(2) == dim && out->stride(2) == 1)
+            to.stride_head = out->stride(1), to.stride_token = out->stride(0);
+        else
+            bad("out: expected [tokens][heads * head_dim] or [tokens][heads][head_dim] with contiguous channels");
+        const double scale = PyFloat_AsDouble(a[9]);
+        if (scale == -1.0 && PyErr_Occurred()) {
+            PyErr_Clear();
+            bad("scale: expected a number");
+        }
+        check(g_abi.attention(b, (int32_t)kind, pages[0], pages[1], tq, to, scale, stream_of(a[10], device)));
+        return wrap(out, a[8]);
+    });
+}
+
+PyMethodDef kMethods[] = {{"bind", (PyCFunction)(void*)bind, METH_FASTCALL, nullptr},
+                          {"norm_rotate", (PyCFunction)(void*)norm_rotate, METH_FASTCALL, nullptr},
+                          {"norm_rotate_backward", (PyCFunction)(void*)norm_rotate_backward, METH_FASTCALL, nullptr},
+                          {"append", (PyCFunction)(void*)append, METH_FASTCALL, nullptr},
+                          {"attention", (PyCFunction)(void*)attention, METH_FASTCALL, nullptr},
+                          {nullptr, nullptr, 0, nullptr}};
+PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_kv_cache_calls", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__kv_cache_calls() { return PyModule_Create(&kModule); }

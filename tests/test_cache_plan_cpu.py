@@ -9,6 +9,12 @@ import pytest
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    from paper_2511_21317_b200 import build
+    build.build()
+
+
 @pytest.fixture(scope="module")
 def program(tmp_path_factory):
     gxx = shutil.which("g++")

@@ -343,3 +343,26 @@ def test_refusals():
         none.norm_rotate(q, k, pos, w[0])
     rot.close()
     refuses(-1, q, k, pos)
+
+
+def test_refusals_of_the_gradients():
+    q, k, pos, w, b, rot = make(64, "layer", 2, 64, False, 20, 4, 4, torch.bfloat16, "heads", seed=9)
+
+    def refuses(code, *a, **kw):
+        with pytest.raises(hb.HttmError) as e:
+            rot.norm_rotate_backward(*a, **kw)
+        assert e.value.code == code, str(e.value)
+
+    refuses(-1, None, None, None, None, pos)
+    refuses(-1, None, k, q, k, pos)                                # no gradient of q's output
+    refuses(-1, q.float(), None, q, None, pos)
+    refuses(-1, q[:, :19], None, q, None, pos)
+    refuses(-1, q, None, q, None, None)
+    refuses(-1, q, None, q, None, pos, w[0].double())
+    refuses(-1, q, None, q, None, pos, out_q=torch.empty(4, 20, 65, dtype=torch.bfloat16, device=DEV)[..., :63])
+    refuses(-1, "q", None, q, None, pos)
+    base = torch.zeros(4 * 20 * 64 + 4096, dtype=torch.bfloat16, device=DEV)
+    refuses(-1, base[:5120].view(4, 20, 64), None, q, None, pos, out_q=base[1024:6144].view(4, 20, 64))
+    assert rot.norm_rotate_backward(q, None, q, None, pos)[1:] == (None,) * 5
+    with pytest.raises(TypeError):
+        rot.norm_rotate_backward(q)
