@@ -247,7 +247,6 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
     OnDevice guard(c.device);
     if (!guard.ok) return global_fail(HTTM_ERR_CUDA, "cache_attention: cudaSetDevice failed");
     CacheArgs a{};
-    a.segs = part_of<CacheSeg>(b, b->at.segs);
     a.jobs = part_of<CacheJob>(b, b->at.narrow_jobs);
     a.job_start = part_of<int32_t>(b, b->at.narrow_start);
     a.table = part_of<int32_t>(b, b->at.table);
@@ -262,6 +261,7 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
     a.kv_heads = c.kv_heads;
     a.page_shift = p.page_shift;
     a.n_tokens = p.n_tokens;
+    a.causal = c.causal;
     a.status = b->status;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (!p.wide_jobs.empty()) {

@@ -23,11 +23,16 @@ struct BatchInput {
     const int32_t* prefix_pages;
     int32_t prefix_length;
 };
+// A row tile and the keys its rows see.
+struct RowTile {
+    int32_t token0, tokens, tile_rows;
+    int32_t prefix_keys, own_keys, own_table, seen0;   // see CacheJob
+};
 struct BatchPlan {
     int32_t n_tokens = 0, page_shift = 0, part_units = 0;
     int64_t last_position = -1;       // largest place of a new token behind the prefix
     bool can_append = true, same_place = false;
-    std::vector<CacheSeg> segs;
+    std::vector<RowTile> segs;
     std::vector<CacheJob> narrow_jobs, wide_jobs;
     std::vector<int32_t> narrow_start, wide_start;   // [CTAs + 1]
     std::vector<int32_t> table, prefix_seg, own_seg, slots, positions;
@@ -93,14 +98,18 @@ struct Dealer {
     int kv_heads;
     void take(int cta, const BatchItem& it, int t0, int t1, bool whole) {
         CacheJob j{};
-        j.seg = it.seg, j.head = it.head, j.pair = it.pair, j.tile0 = t0, j.tile1 = t1;
-        j.part = j.part2 = -1;
+        const RowTile& first = p->segs[it.seg];
+        j.tile_rows = first.tile_rows, j.pair = it.pair, j.head = it.head, j.tile0 = t0, j.tile1 = t1;
+        j.token0 = first.token0, j.prefix_keys = first.prefix_keys, j.own_table = first.own_table;
+        j.part[0] = j.part[1] = -1;
         for (int k = 0; k <= it.pair; ++k) {
+            const RowTile& s = p->segs[it.seg + k];
+            j.tokens[k] = s.tokens, j.own_keys[k] = s.own_keys, j.seen0[k] = s.seen0;
             int2& parts = p->parts[(size_t)(it.seg + k) * kv_heads + it.head];
             if (whole) {
                 parts.y = -1;
             } else {
-                (k ? j.part2 : j.part) = parts.x + parts.y * (p->segs[it.seg + k].tile_rows / kPartUnit);
+                j.part[k] = parts.x + parts.y * (s.tile_rows / kPartUnit);
                 ++parts.y;
             }
         }
@@ -240,16 +249,15 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     std::vector<BatchItem> narrow, wide;
     std::vector<std::pair<int, int>> pairs;   // wide: (row tile, 1 if the next one goes with it)
     std::vector<char> sole;
-    auto key_tiles = [&](const CacheSeg& s, int keys) { return (s.prefix_keys + keys - 1) / keys + (s.own_keys + keys - 1) / keys; };
+    auto key_tiles = [&](const RowTile& s, int keys) { return (s.prefix_keys + keys - 1) / keys + (s.own_keys + keys - 1) / keys; };
     auto add = [&](int32_t token0, int32_t tokens, int rows, int32_t prefix_keys, int seq, int32_t first_query) {
-        CacheSeg s{};
+        RowTile s{};
         s.token0 = token0, s.tokens = tokens, s.tile_rows = rows, s.prefix_keys = prefix_keys;
         if (seq >= 0) {
             const int32_t length = in.lengths[seq];
             s.own_table = table_at[seq];
             s.seen0 = c.causal ? length - in.queries[seq] + first_query + 1 : length;
-            s.seen_step = c.causal;
-            s.own_keys = std::max<int32_t>(0, std::min<int64_t>(length, (int64_t)s.seen0 + (int64_t)(tokens - 1) * s.seen_step));
+            s.own_keys = std::max<int32_t>(0, std::min<int64_t>(length, (int64_t)s.seen0 + (c.causal ? tokens - 1 : 0)));
         }
         if (s.prefix_keys == 0 && s.own_keys == 0) return;
         const int at = (int)p->segs.size();
@@ -288,7 +296,7 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     // Two row tiles of 128 rows form a pair if they look at the same keys (a pair walks those of the second one, which sees at least as many) and are dealt
     // alike; a pair's key tile takes twice as long as a single's.
     for (int s = 0; s < (int)p->segs.size(); ++s) {
-        const CacheSeg& a = p->segs[s];
+        const RowTile& a = p->segs[s];
         if (a.tile_rows != kWideRows) continue;
         const bool pair = s + 1 < (int)p->segs.size() && p->segs[s + 1].tile_rows == kWideRows && p->segs[s + 1].prefix_keys == a.prefix_keys &&
                           (p->segs[s + 1].own_keys > 0) == (a.own_keys > 0) && p->segs[s + 1].own_table == a.own_table &&
@@ -343,7 +351,7 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
 
 // Where the parts of a plan lie in one block (offsets in bytes, multiples of 256).
 struct BatchLayout {
-    size_t segs = 0, narrow_jobs = 0, wide_jobs = 0, narrow_start = 0, wide_start = 0, table = 0, combine_tasks = 0, slots = 0, positions = 0, bytes = 0;
+    size_t narrow_jobs = 0, wide_jobs = 0, narrow_start = 0, wide_start = 0, table = 0, combine_tasks = 0, slots = 0, positions = 0, bytes = 0;
     BatchLayout() = default;
     explicit BatchLayout(const BatchPlan& p) {
         auto room = [&](size_t n) {
@@ -352,7 +360,7 @@ struct BatchLayout {
             return at;
         };
         auto of = [&](const auto& v) { return room(v.size() * sizeof(v[0])); };
-        segs = of(p.segs), narrow_jobs = of(p.narrow_jobs), wide_jobs = of(p.wide_jobs), narrow_start = of(p.narrow_start), wide_start = of(p.wide_start);
+        narrow_jobs = of(p.narrow_jobs), wide_jobs = of(p.wide_jobs), narrow_start = of(p.narrow_start), wide_start = of(p.wide_start);
         table = of(p.table), combine_tasks = of(p.combine_tasks), slots = of(p.slots), positions = of(p.positions);
         bytes += 256;
     }
@@ -360,7 +368,7 @@ struct BatchLayout {
         auto put = [&](size_t at, const auto& v) {
             if (!v.empty()) memcpy(to + at, v.data(), v.size() * sizeof(v[0]));
         };
-        put(segs, p.segs), put(narrow_jobs, p.narrow_jobs), put(wide_jobs, p.wide_jobs), put(narrow_start, p.narrow_start), put(wide_start, p.wide_start);
+        put(narrow_jobs, p.narrow_jobs), put(wide_jobs, p.wide_jobs), put(narrow_start, p.narrow_start), put(wide_start, p.wide_start);
         put(table, p.table), put(combine_tasks, p.combine_tasks), put(slots, p.slots), put(positions, p.positions);
     }
 };

@@ -98,23 +98,21 @@ constexpr int kWideRows = 128;     // query rows of a tile of the wide kernel; t
 inline int narrow_ctas_per_sm(int head_dim) { return head_dim == 64 ? 3 : 2; }
 constexpr int kPartUnit = 16;      // partial results are laid out in units of 16 rows of head_dim + 2 floats
 
-// A row tile and the keys its rows see.  Rows are (token, query head of the group), the group's heads of a token side by side.
-struct alignas(16) CacheSeg {
-    int32_t token0, tokens;     // the tokens of the tile
+// A job: key tiles [tile0, tile1) of a row tile and a key head, those of the prefix first, then the own ones.  Rows are (token, query head of the group), the
+// group's heads of a token side by side.  Everything that a kernel has to know of its job is in this one record: it is one trip to memory away.
+struct alignas(16) CacheJob {
     int32_t tile_rows;          // 16, 32, 64: narrow; 128: wide
-    int32_t prefix_keys;        // keys of the prefix (0: this tile does not look at it)
-    int32_t own_keys;           // most own keys that any of its tokens sees (0: none)
+    int32_t pair;               // wide: 1 if the job takes the row tile behind this one too ([1] below)
+    int32_t head, tile0, tile1;
+    int32_t part[2];            // first unit of the partial result; -1: it is the whole result and goes to `out`
+    int32_t token0;             // the row tile's first token; the second one's follow the first one's
+    int32_t tokens[2];
+    int32_t prefix_keys;        // keys of the prefix (0: these rows do not look at it)
+    int32_t own_keys[2];        // most own keys that any token of the row tile sees (0: none)
+    int32_t seen0[2];           // token i of the row tile sees min(own_keys, seen0 + i) own keys if causal, min(own_keys, seen0) if not
     int32_t own_table;          // where the sequence's pages begin in the table
-    int32_t seen0, seen_step;   // token i of the tile sees min(own_keys, seen0 + i * seen_step) own keys
 };
-struct alignas(16) CacheJob {   // key tiles [tile0, tile1) of a row tile: those of the prefix, then the own ones
-    int32_t seg, head;
-    int32_t pair;               // wide: 1 if the job takes the row tile behind `seg` too
-    int32_t tile0, tile1;
-    int32_t part;               // first unit of its partial result; -1: it is the whole result and goes to `out`
-    int32_t part2;              // of the second row tile
-    int32_t pad;
-};
+static_assert(sizeof(CacheJob) == 64, "four 16-byte words");
 constexpr int kCombineWarps = 8, kCombineRows = 8, kCombineFewRows = 2, kCombineManyParts = 16;
 struct alignas(16) CombineTask {   // rows of one key head whose partial results are to be added up
     int32_t token0, first_head;    // the first row: token, head of the group; the others follow, the group's heads of a token side by side
@@ -125,7 +123,6 @@ struct alignas(16) CombineTask {   // rows of one key head whose partial results
     int32_t unit[2], parts[2], tile_rows[2], row[2];
 };
 struct CacheArgs {
-    const CacheSeg* segs;
     const CacheJob* jobs;
     const int32_t* job_start;   // [CTAs + 1]
     const int32_t* table;       // pages of the prefix, then of every sequence
@@ -136,7 +133,7 @@ struct CacheArgs {
     int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
     float* partial;
     float scale_log2;
-    int32_t group, kv_heads, page_shift, n_tokens;
+    int32_t group, kv_heads, page_shift, n_tokens, causal;
     int32_t early;              // narrow: the kernel in front belongs to the same call, inputs may be read while it runs
     int32_t* status;
 };

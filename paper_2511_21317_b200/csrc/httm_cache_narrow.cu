@@ -69,7 +69,6 @@ struct Shared {
     float merge[4][16][kMergeChannels + 4];   // [warp][row]; the pitch keeps rows on distinct banks
     float2 stats[4][16];
     CacheJob jobs[kRecords];
-    CacheSeg segs[kRecords];
 };
 template <typename T, int D>
 struct Stream {
@@ -102,10 +101,10 @@ struct Stream {
         } else {
             keys = 0;
             if (++job >= n_jobs) return;
-            const int tile = sm.jobs[job].tile0, prefix = sm.segs[job].prefix_keys, n_prefix = (prefix + kNarrowKeys - 1) / kNarrowKeys;
+            const int tile = sm.jobs[job].tile0, prefix = sm.jobs[job].prefix_keys, n_prefix = (prefix + kNarrowKeys - 1) / kNarrowKeys;
             left = sm.jobs[job].tile1 - tile - 1;
             head = sm.jobs[job].head;
-            own_keys = sm.segs[job].own_keys, own_table = sm.segs[job].own_table;
+            own_keys = sm.jobs[job].own_keys[0], own_table = sm.jobs[job].own_table;
             more = tile < n_prefix;
             key0 = (more ? tile : tile - n_prefix) * kNarrowKeys;
             end = more ? prefix : own_keys;
@@ -152,11 +151,11 @@ struct Stream {
 
 // One job with a tile of 16 MT rows.  Warp w has rows 16 (w mod MT) .. and of every key tile the keys 16 MT (w / MT) .. .
 template <typename T, int D, int MT>
-__device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg seg, const CacheJob job, Shared<D>& sm, Stream<T, D>& stream) {
+__device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheJob job, Shared<D>& sm, Stream<T, D>& stream) {
     constexpr int KG = 4 / MT, NB = 2 * MT;   // warps that share a row by keys; blocks of eight keys of a warp
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int row0 = (warp % MT) * 16 + (lane >> 2), key_base = (warp / MT) * 16 * MT;
-    const int n_rows = seg.tokens * a.group;
+    const int n_rows = job.tokens[0] * a.group;
 
     // rows as operands of the matrix instruction: this thread has rows row0 and row0 + 8
     uint32_t qf[D / 16][4];
@@ -166,8 +165,8 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg se
         const int row = row0 + 8 * r;
         const bool valid = row < n_rows;
         const int token = valid ? row / a.group : 0;
-        seen[r] = min(seg.own_keys, seg.seen0 + token * seg.seen_step);
-        const T* q = static_cast<const T*>(a.q) + (int64_t)(seg.token0 + token) * a.q_token + (int64_t)(job.head * a.group + (valid ? row % a.group : 0)) * a.q_head +
+        seen[r] = min(job.own_keys[0], job.seen0[0] + (a.causal ? token : 0));
+        const T* q = static_cast<const T*>(a.q) + (int64_t)(job.token0 + token) * a.q_token + (int64_t)(job.head * a.group + (valid ? row % a.group : 0)) * a.q_head +
                      2 * (lane & 3);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
@@ -180,11 +179,11 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg se
     for (int c = 0; c < D / 8; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
-    const int n_prefix = (seg.prefix_keys + kNarrowKeys - 1) / kNarrowKeys;
+    const int n_prefix = (job.prefix_keys + kNarrowKeys - 1) / kNarrowKeys;
     for (int i = job.tile0; i < job.tile1; ++i) {
         const uint32_t ks = stream.next(), vs = ks + kNarrowKeys * D * 2;
         const bool own = i >= n_prefix;
-        const int key0 = (own ? i - n_prefix : i) * kNarrowKeys, keys = (own ? seg.own_keys : seg.prefix_keys) - key0;
+        const int key0 = (own ? i - n_prefix : i) * kNarrowKeys, keys = (own ? job.own_keys[0] : job.prefix_keys) - key0;
         float s[NB][4];
 #pragma unroll
         for (int b = 0; b < NB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
@@ -265,7 +264,7 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg se
         __syncthreads();
         for (int i = tid; i < 16 * MT * QUADS; i += kThreads) {
             // the result is stored row by row, parts quad by quad (see cache_combine_kernel)
-            const int row = job.part < 0 ? i / QUADS : i % (16 * MT), c = job.part < 0 ? i % QUADS : i / (16 * MT);
+            const int row = job.part[0] < 0 ? i / QUADS : i % (16 * MT), c = job.part[0] < 0 ? i % QUADS : i / (16 * MT);
             if (row >= n_rows) continue;
             float top = -INFINITY;
 #pragma unroll
@@ -280,13 +279,13 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheSeg se
                 sum.x = fmaf(v.x, f, sum.x), sum.y = fmaf(v.y, f, sum.y), sum.z = fmaf(v.z, f, sum.z), sum.w = fmaf(v.w, f, sum.w);
                 total = fmaf(st.y, f, total);
             }
-            if (job.part < 0) {
+            if (job.part[0] < 0) {
                 const float inv = top == -INFINITY ? 0.f : 1.f / total;
-                T* out = static_cast<T*>(a.out) + (int64_t)(seg.token0 + row / a.group) * a.out_token + (int64_t)(job.head * a.group + row % a.group) * a.out_head +
+                T* out = static_cast<T*>(a.out) + (int64_t)(job.token0 + row / a.group) * a.out_token + (int64_t)(job.head * a.group + row % a.group) * a.out_head +
                          c0 + 4 * c;
                 *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum.x * inv, sum.y * inv), pack2<T>(sum.z * inv, sum.w * inv));
             } else {
-                float* to = a.partial + (int64_t)job.part * (kPartUnit * (D + 2));
+                float* to = a.partial + (int64_t)job.part[0] * (kPartUnit * (D + 2));
                 __stcg(reinterpret_cast<float4*>(to) + (c0 / 4 + c) * 16 * MT + row, sum);
                 if (c0 == 0 && c == 0) __stcg(reinterpret_cast<float2*>(to + 16 * MT * D + 2 * row), make_float2(top, total));
             }
@@ -303,13 +302,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) cache_narrow_kernel
     for (int j0 = (int)ld_l2(a.job_start + blockIdx.x); j0 < last; j0 += kRecords) {
         const int n = min(kRecords, last - j0);
         __syncthreads();   // (the records before these have been read)
-        if (threadIdx.x < 2 * n) {
-            const int j = threadIdx.x >> 1, half = threadIdx.x & 1;
-            const int4 v = ld_l2_16(reinterpret_cast<const int4*>(a.jobs + j0 + j) + half);
-            reinterpret_cast<int4*>(sm.jobs + j)[half] = v;
-            const int seg = __shfl_sync(__activemask(), v.x, threadIdx.x & 30);   // (the first word of a job)
-            reinterpret_cast<int4*>(sm.segs + j)[half] = ld_l2_16(reinterpret_cast<const int4*>(a.segs + seg) + half);
-        }
+        if (threadIdx.x < 4 * n) reinterpret_cast<int4*>(sm.jobs)[threadIdx.x] = ld_l2_16(reinterpret_cast<const int4*>(a.jobs + j0) + threadIdx.x);
         __syncthreads();
         Stream<T, D> stream(a, sm, n);
         if (!waited) {
@@ -319,13 +312,13 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) cache_narrow_kernel
         }
         stream.start();
         for (int j = 0; j < n; ++j) {
-            const int rows = sm.segs[j].tile_rows;
+            const int rows = sm.jobs[j].tile_rows;
             if (rows == 16)
-                narrow_job<T, D, 1>(a, sm.segs[j], sm.jobs[j], sm, stream);
+                narrow_job<T, D, 1>(a, sm.jobs[j], sm, stream);
             else if (rows == 32)
-                narrow_job<T, D, 2>(a, sm.segs[j], sm.jobs[j], sm, stream);
+                narrow_job<T, D, 2>(a, sm.jobs[j], sm, stream);
             else
-                narrow_job<T, D, 4>(a, sm.segs[j], sm.jobs[j], sm, stream);
+                narrow_job<T, D, 4>(a, sm.jobs[j], sm, stream);
         }
         copies_wait<0>();
     }
@@ -365,8 +358,9 @@ __device__ __forceinline__ void combine_rows(const CacheArgs& a, const CombineTa
 #pragma unroll
                 for (int c = 0; c < Q; ++c) v[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (p < n) {
-                    const int k = p < n0 ? 0 : 1, tile_rows = task.tile_rows[k], at = task.row[k] + row;
-                    const float* part = base[k] + (p - (k ? n0 : 0)) * stride[k];
+                    const bool own = p >= n0;
+                    const int tile_rows = own ? task.tile_rows[1] : task.tile_rows[0], at = (own ? task.row[1] : task.row[0]) + row;
+                    const float* part = own ? base[1] + (p - n0) * stride[1] : base[0] + p * stride[0];
                     st[i] = __ldcg(reinterpret_cast<const float2*>(part + tile_rows * D) + at);
 #pragma unroll
                     for (int c = 0; c < Q; ++c) v[i][c] = __ldcg(reinterpret_cast<const float4*>(part) + (quad + STEP * c) * tile_rows + at);

@@ -81,15 +81,14 @@ __device__ __forceinline__ uint32_t uses(int n, int r) {   // how many of 0 .. n
 struct KeyTile {
     int key0, keys;     // first key in the prefix / in the sequence; keys of the tile
     int table;          // where its pages begin in the table
-    bool own;
 };
-__device__ __forceinline__ KeyTile key_tile(const CacheSeg& seg, int tile) {
-    const int n_prefix = (seg.prefix_keys + BN - 1) / BN;
+__device__ __forceinline__ KeyTile key_tile(const CacheJob& job, int tile) {   // (of a pair the second row tile sees the most keys)
+    const int n_prefix = (job.prefix_keys + BN - 1) / BN;
+    const bool own = tile >= n_prefix;
     KeyTile t;
-    t.own = tile >= n_prefix;
-    t.key0 = (t.own ? tile - n_prefix : tile) * BN;
-    t.keys = min(BN, (t.own ? seg.own_keys : seg.prefix_keys) - t.key0);
-    t.table = t.own ? seg.own_table : 0;
+    t.key0 = (own ? tile - n_prefix : tile) * BN;
+    t.keys = min(BN, (own ? (job.pair ? job.own_keys[1] : job.own_keys[0]) : job.prefix_keys) - t.key0);
+    t.table = own ? job.own_table : 0;
     return t;
 }
 
@@ -215,11 +214,9 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         bool ok = true;
         for (int j = job_first; ok && j < job_last; ++j) {
             const CacheJob job = ld_record(a.jobs + j);
-            const CacheSeg seg = ld_record(a.segs + job.seg + job.pair);   // (of a pair the second row tile sees the most keys)
-            const int token_a = job.pair ? seg.token0 - BM / a.group : seg.token0;
             const int n = job.tile1 - job.tile0;
             auto page_of = [&](int i) {   // of this lane's box of key tile i
-                const KeyTile t = key_tile(seg, job.tile0 + i);
+                const KeyTile t = key_tile(job, job.tile0 + i);
                 const int p = lane / SUB;
                 return p * box < t.keys ? (int32_t)ld_l2(a.table + t.table + (t.key0 >> a.page_shift) + p) : -1;
             };
@@ -234,7 +231,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     tc::mbar_expect_tx(bar(bars->q_full), job.pair ? 2 * q_bytes : q_bytes);
                     for (int x = 0; x <= job.pair; ++x)
                         for (int c = 0; c < SUB; ++c)
-                            tma_load_4d(s_q + x * TILE + c * kSubTile, &map_q, bar(bars->q_full), 64 * c, 0, job.pair && x == 0 ? token_a : seg.token0, job.head);
+                            tma_load_4d(s_q + x * TILE + c * kSubTile, &map_q, bar(bars->q_full), 64 * c, 0, job.token0 + (x ? job.tokens[0] : 0), job.head);
                 }
                 ++q_loads;
             }
@@ -245,7 +242,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     const int i = i0 + st;
                     if (!ok || i >= n) break;
                     const uint32_t fill = base[st] + (uint32_t)(i0 / NB);
-                    const KeyTile t = key_tile(seg, job.tile0 + i);
+                    const KeyTile t = key_tile(job, job.tile0 + i);
                     const int boxes = (t.keys + box - 1) / box, slot = t.key0 & (page - 1);   // (pages of 256: one of two halves)
                     const bool tail = is_v && t.keys < BN;
                     const uint32_t b = tail ? bar(bars->v_tail) : bar(full[st]);
@@ -420,27 +417,35 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         uint32_t sp_bits = 0, od_base = 0, singles = 0;   // before this job: parity of each score buffer's completions; the group's P V; singles
         float2* xch = reinterpret_cast<float2*>(smem + (2 + 2 * NB) * TILE + 512);
         const float c = fmaxf(fabsf(a.scale_log2), 1e-30f);   // (not 0: a masked score is -inf, and stays so)
+        // What the loop over the key tiles has to know of a job (few registers are left beside the scores; what its end needs is read again there, together
+        // with the next job's record).
+        struct View {
+            int n_score, n_own, tile0, prefix_keys, n_prefix, seen_to;
+            bool pair, exists;
+        };
+        auto view = [&](const CacheJob& job) {
+            const int n = job.tile1 - job.tile0, token = row / a.group;
+            const bool second = job.pair && x == 1;
+            const int own_keys = second ? job.own_keys[1] : job.own_keys[0], seen0 = second ? job.seen0[1] : job.seen0[0];
+            View u;
+            u.pair = job.pair != 0;
+            u.n_score = u.pair ? 2 * n : n;
+            u.n_own = u.pair ? n : (n - x + 1) / 2;
+            u.tile0 = job.tile0;
+            u.prefix_keys = job.prefix_keys;
+            u.n_prefix = (job.prefix_keys + BN - 1) / BN;
+            u.exists = token < (second ? job.tokens[1] : job.tokens[0]);
+            // own keys that the row sees, counted like the tiles: behind the prefix's last, which is filled up (a row that does not exist sees all of them)
+            u.seen_to = u.n_prefix * BN + (u.exists ? min(own_keys, seen0 + (a.causal ? token : 0)) : own_keys);
+            return u;
+        };
+        View v = view(ld_record(a.jobs + job_first));
+        depend_wait();   // partial results and `out` are free to be written
         bool ok = true;
         int jobs = 0;
         for (int jb = job_first; ok && jb < job_last; ++jb, ++jobs) {
-            // (few registers are left beside the scores: what only the job's end needs is read again there)
-            int n_score, n_own, tile0, n_prefix, prefix_keys, seen_to, tokens;
-            bool pair;
-            {
-                const CacheJob job = ld_record(a.jobs + jb);
-                const CacheSeg seg = ld_record(a.segs + job.seg + (job.pair ? x : 0));
-                if (jb == job_first) depend_wait();   // (partial results and `out` are free to be written)
-                const int n = job.tile1 - job.tile0, token = row / a.group;
-                pair = job.pair != 0;
-                n_score = pair ? 2 * n : n;
-                n_own = pair ? n : (n - x + 1) / 2;
-                tile0 = job.tile0;
-                prefix_keys = seg.prefix_keys;
-                n_prefix = (prefix_keys + BN - 1) / BN;
-                tokens = seg.tokens;
-                // own keys that the row sees, counted like the tiles: behind the prefix's last, which is filled up (a row that does not exist sees all of them)
-                seen_to = n_prefix * BN + (token < seg.tokens ? min(seg.own_keys, seg.seen0 + token * seg.seen_step) : seg.own_keys);
-            }
+            const int n_score = v.n_score, n_own = v.n_own, tile0 = v.tile0, prefix_keys = v.prefix_keys, n_prefix = v.n_prefix, seen_to = v.seen_to;
+            const bool pair = v.pair, exists = v.exists;
             float m = -INFINITY, l = 0.f;
             {   // the accumulator starts at zero: every P V adds to it (ordered before the first arrival at p_full)
                 uint32_t z[32];
@@ -450,7 +455,6 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 for (int c = 0; c < D; c += 32) tc::tmem_st32(t_o + c, z);
                 if (n_own == 0) tc::tmem_wait_st();
             }
-            const bool exists = row / a.group < tokens;
             // The accumulator times f, once the group's last P V is done (the next is issued behind the P of the tile at hand).
             auto rescale = [&](float f, uint32_t j) {
                 if (!__all_sync(0xffffffffu, tc::mbar_wait(bar(bars->o_done[x]), (od_base + j - 1) & 1u, abort_flag))) return false;
@@ -569,12 +573,11 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 if (!kHalf && __any_sync(0xffffffffu, exists && tile_sum >= kSumLimit)) {   // (a sum that is not a number stays one)
                     const bool mine = exists && tile_sum >= kSumLimit;
                     const CacheJob job = ld_record(a.jobs + jb);
-                    const CacheSeg seg = ld_record(a.segs + job.seg + (pair ? x : 0));
-                    const int token = mine ? row / a.group : 0, gi = mine ? row % a.group : 0;
-                    const T* q_row = static_cast<const T*>(a.q) + (int64_t)(seg.token0 + token) * a.q_token + (int64_t)(job.head * a.group + gi) * a.q_head;
+                    const int token = job.token0 + (pair && x ? job.tokens[0] : 0) + (mine ? row / a.group : 0);
+                    const T* q_row = static_cast<const T*>(a.q) + (int64_t)token * a.q_token + (int64_t)(job.head * a.group + (mine ? row % a.group : 0)) * a.q_head;
                     const bool own = tile >= n_prefix;
                     tc::tmem_wait_st();
-                    const float2 again = redo_tile<T, D>(a, mine ? q_row : nullptr, job.head, own ? seg.own_table : 0, (own ? tile - n_prefix : tile) * BN,
+                    const float2 again = redo_tile<T, D>(a, mine ? q_row : nullptr, job.head, own ? job.own_table : 0, (own ? tile - n_prefix : tile) * BN,
                                                          min(limit, BN), m, t_s + kPColumn);
                     float f = 1.f;
                     if (mine) {
@@ -590,13 +593,15 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 tc::fence_before_sync();
                 tc::mbar_arrive(p_full);
             }
-            if (ok && !pair && x == 1) {
+            if (!ok) break;
+            const CacheJob job = ld_record(a.jobs + jb), next = ld_record(a.jobs + min(jb + 1, job_last - 1));
+            if (!pair && x == 1) {
                 // single, group B: this row's (maximum, sum); O_B stays in tensor memory until group A has read it
                 xch[row] = make_float2(m, l);
                 tc::fence_before_sync();
                 tc::mbar_arrive(bar(bars->x_full));
                 ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->x_done), singles & 1u, abort_flag));
-            } else if (ok) {
+            } else {
                 ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->o_final), (uint32_t)jobs & 1u, abort_flag));
                 if (ok && !pair) ok = __all_sync(0xffffffffu, tc::mbar_wait(bar(bars->x_full), singles & 1u, abort_flag));
                 if (!ok) break;
@@ -611,16 +616,15 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     l = l * fa + pb.y * fb;
                     m = mm;
                 }
-                const CacheJob job = ld_record(a.jobs + jb);
-                const CacheSeg seg = ld_record(a.segs + job.seg + (pair ? x : 0));
-                const int part = x == 0 ? job.part : job.part2, token = row / a.group, head = job.head * a.group + row % a.group;
-                const bool exists = token < seg.tokens;
+                const bool second = pair && x == 1;
+                const int part = second ? job.part[1] : job.part[0], head = job.head * a.group + row % a.group;
+                const int token = job.token0 + (second ? job.tokens[0] : 0) + row / a.group;
                 if (part < 0) {
                     const float inv = m == -INFINITY ? 0.f : 1.f / l;
                     fa *= inv;
                     fb *= inv;
                 }
-                T* out = static_cast<T*>(a.out) + (int64_t)(seg.token0 + token) * a.out_token + (int64_t)head * a.out_head;
+                T* out = static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head;
                 float* to = a.partial + (int64_t)part * (kPartUnit * (D + 2));
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
@@ -664,6 +668,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             if (!pair) ++singles;
 #pragma unroll
             for (int b = 0; b < NB; ++b) sp_bits ^= (uses<NB>(n_score, b) & 1u) << b;
+            v = view(next);
         }
     }
     tc::fence_before_sync();

@@ -68,13 +68,13 @@ static bool one_round() {
             for (int which : {p.prefix_seg[t], p.own_seg[t]}) {
                 if (which < 0) continue;
                 NEED(which < (int)p.segs.size());
-                const CacheSeg& s = p.segs[which];
+                const RowTile& s = p.segs[which];
                 NEED(t >= s.token0 && t < s.token0 + s.tokens && s.tokens * group <= s.tile_rows);
                 NEED(s.tile_rows == 16 || s.tile_rows == 32 || s.tile_rows == 64 || s.tile_rows == kWideRows);
                 NEED(s.prefix_keys == 0 || s.prefix_keys == prefix);
                 shared += s.prefix_keys;
                 if (s.own_keys > 0) {
-                    own += std::max(0, std::min(s.own_keys, s.seen0 + (t - s.token0) * s.seen_step));
+                    own += std::max(0, std::min(s.own_keys, s.seen0 + (c.causal ? t - s.token0 : 0)));
                     for (int k = 0; k < pages_of(s.own_keys, c.page_size); ++k) {
                         NEED(s.own_table + k < (int)p.table.size());
                         NEED(p.table[s.own_table + k] == tables[(size_t)i * stride + k]);
@@ -100,20 +100,28 @@ static bool one_round() {
         NEED((int)start.size() - 1 <= (wide ? 1 : narrow_ctas_per_sm(c.head_dim)) * sms && start[0] == 0 && start.back() == (int)jobs.size());
         for (size_t i = 1; i < start.size(); ++i) NEED(start[i] > start[i - 1]);
         for (const CacheJob& j : jobs) {
-            NEED(j.seg >= 0 && j.seg + j.pair < (int)p.segs.size() && j.head >= 0 && j.head < c.kv_heads && j.pair >= 0 && j.pair <= wide);
-            NEED(j.tile0 >= 0 && j.tile1 > j.tile0);
-            for (int k = 0; k <= j.pair; ++k) {
-                NEED((p.segs[j.seg + k].tile_rows == kWideRows) == (wide == 1));
-                auto& of = dealt[std::make_tuple(j.seg + k, j.head)];
+            NEED(j.head >= 0 && j.head < c.kv_heads && j.pair >= 0 && j.pair <= wide);
+            NEED(j.tile0 >= 0 && j.tile1 > j.tile0 && (j.tile_rows == kWideRows) == (wide == 1));
+            int token = j.token0;
+            for (int k = 0; k <= j.pair; ++k) {   // the record holds what its row tiles are
+                NEED(token >= 0 && token < tokens);
+                const int at[2] = {p.prefix_seg[token], p.own_seg[token]};
+                const int s = j.own_keys[k] > 0 ? at[1] : at[0] >= 0 ? at[0] : at[1];
+                NEED(s >= 0);
+                const RowTile& seg = p.segs[s];
+                NEED(seg.token0 == token && seg.tokens == j.tokens[k] && seg.tile_rows == j.tile_rows && seg.prefix_keys == j.prefix_keys);
+                NEED(seg.own_keys == j.own_keys[k] && (seg.own_keys == 0 || (seg.own_table == j.own_table && seg.seen0 == j.seen0[k])));
+                auto& of = dealt[std::make_tuple(s, j.head)];
                 NEED(of.count(j.tile0) == 0);
-                of[j.tile0] = {j.tile1, k ? j.part2 : j.part};
+                of[j.tile0] = {j.tile1, j.part[k]};
+                token += j.tokens[k];
             }
         }
     }
     std::set<std::pair<int, int>> ranges;   // of partial results
     for (int s = 0; s < (int)p.segs.size(); ++s)
         for (int h = 0; h < c.kv_heads; ++h) {
-            const CacheSeg& seg = p.segs[s];
+            const RowTile& seg = p.segs[s];
             const int keys = seg.tile_rows == kWideRows ? kWideKeys : kNarrowKeys, units = seg.tile_rows / kPartUnit;
             const int2 parts = p.parts[(size_t)s * c.kv_heads + h];
             int at = 0, n = 0, end = 0;
@@ -170,7 +178,7 @@ static bool one_round() {
     const BatchLayout at(p);
     std::vector<unsigned char> block(at.bytes, 0);
     at.write(p, block.data());
-    NEED(p.segs.empty() || memcmp(block.data() + at.segs, p.segs.data(), p.segs.size() * sizeof(CacheSeg)) == 0);
+    NEED(p.wide_jobs.empty() || memcmp(block.data() + at.wide_jobs, p.wide_jobs.data(), p.wide_jobs.size() * sizeof(CacheJob)) == 0);
     NEED(p.positions.empty() || memcmp(block.data() + at.positions, p.positions.data(), p.positions.size() * 4) == 0);
     return true;
 }
