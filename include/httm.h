@@ -412,7 +412,7 @@ typedef struct {
 } httm_rows_grad;
 
 /* The gradients of httm_norm_rotate.  Those of weight and bias are sums over all rows, in 32 bits and in an order that depends on
- * the sizes alone: the same call gives the same bits.  UNSUPPORTED for more than 8192 heads of q and k together. */
+ * the sizes alone: the same call gives the same bits.  UNSUPPORTED for more than 1024 heads of q and k together. */
 int httm_norm_rotate_backward(httm_rotary* rotary, int32_t dtype, int64_t n_tokens, const int32_t* positions,
                               const httm_rows_grad* q, const httm_rows_grad* k, void* cuda_stream);
 

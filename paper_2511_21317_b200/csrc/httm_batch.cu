@@ -9,9 +9,11 @@
 #include <algorithm>
 #include <cmath>
 #include <exception>
+#include <mutex>
 #include <new>
 #include <string>
 #include <utility>
+#include <vector>
 
 #include "httm_batch_plan.h"
 #include "httm_cache.h"
@@ -25,15 +27,15 @@ struct httm_batch {
     BatchPlan plan;
     BatchLayout at;                  // where the parts of the plan lie in `data`
     bool set = false;
-    unsigned char* data = nullptr;   // device copy of the plan
+    unsigned char* data = nullptr;   // device copy of the plan, and behind it room for partial results
     unsigned char* staged = nullptr; // pinned
     size_t data_bytes = 0, staged_bytes = 0;
-    float* partial = nullptr;
-    size_t partial_floats = 0;
+    int64_t sets = 0;
+    float* partial() const { return reinterpret_cast<float*>(data + at.bytes); }
     int32_t* status = nullptr;
     cudaEvent_t uploaded = nullptr;
     ~httm_batch() {
-        for (void* p : {(void*)data, (void*)partial, (void*)status})
+        for (void* p : {(void*)data, (void*)status})
             if (p) cudaFree(p);
         if (staged) cudaFreeHost(staged);
         if (uploaded) cudaEventDestroy(uploaded);
@@ -68,6 +70,18 @@ int grow(T** p, size_t* have, size_t need, bool pinned) {
     }
     *have = n;
     return HTTM_OK;
+}
+
+// The kernels' shared memory, once per device.
+cudaError_t configure(int device) {
+    static std::mutex mutex;
+    static bool done[64] = {};
+    std::lock_guard<std::mutex> lock(mutex);
+    if (device < 64 && done[device]) return cudaSuccess;
+    cudaError_t e = configure_cache_attention();
+    if (e == cudaSuccess) e = configure_cache_wide();
+    if (e == cudaSuccess && device < 64) done[device] = true;
+    return e;
 }
 
 int check_pages(const httm_pages& t, const httm_batch_config& c, const char* name) {
@@ -124,11 +138,15 @@ int httm_batch_create(const httm_batch_config* config, httm_batch** out) {
     b->cfg = c;
     cudaDeviceGetAttribute(&b->sm_count, cudaDevAttrMultiProcessorCount, c.device);
     int rc = cuda_result(cudaMalloc(reinterpret_cast<void**>(&b->status), sizeof(int32_t)), "batch");
-    if (!rc) rc = cuda_result(cudaMemset(b->status, 0, sizeof(int32_t)), "batch");
+    if (!rc) {
+        SetupStream setup;
+        cudaError_t e = setup.error;
+        if (e == cudaSuccess) e = cudaMemsetAsync(b->status, 0, sizeof(int32_t), setup.stream);
+        if (e == cudaSuccess) e = setup.finish();
+        rc = cuda_result(e, "batch");
+    }
     if (!rc) rc = cuda_result(cudaEventCreateWithFlags(&b->uploaded, cudaEventDisableTiming), "batch");
-    if (!rc) rc = cuda_result(configure_cache_attention(), "batch");
-    if (!rc) rc = cuda_result(configure_cache_wide(), "batch");
-    if (!rc) rc = cuda_result(cudaDeviceSynchronize(), "batch");
+    if (!rc) rc = cuda_result(configure(c.device), "batch");
     if (rc) {
         delete b;
         return rc;
@@ -170,13 +188,21 @@ int httm_batch_set(httm_batch* b, int32_t n_sequences, const int32_t* lengths, c
         OnDevice guard(b->cfg.device);
         if (!guard.ok) return global_fail(HTTM_ERR_CUDA, "batch_set: cudaSetDevice failed");
         b->at = BatchLayout(b->plan);
-        if (int rc = cuda_result(cudaEventSynchronize(b->uploaded), "batch_set")) return rc;   // the last upload has left the staging buffer
-        if (int rc = grow(&b->staged, &b->staged_bytes, b->at.bytes, true)) return rc;
-        if (int rc = grow(&b->data, &b->data_bytes, b->at.bytes, false)) return rc;
-        if (int rc = grow(&b->partial, &b->partial_floats, (size_t)b->plan.part_units * kPartUnit * (b->cfg.head_dim + 2), false)) return rc;
-        b->at.write(b->plan, b->staged);
+        const size_t partial_bytes = (size_t)b->plan.part_units * kPartUnit * (b->cfg.head_dim + 2) * sizeof(float);
+        if (int rc = grow(&b->data, &b->data_bytes, b->at.bytes + partial_bytes, false)) return rc;
         cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-        if (int rc = cuda_result(cudaMemcpyAsync(b->data, b->staged, b->at.bytes, cudaMemcpyHostToDevice, stream), "batch_set: upload")) return rc;
+        std::vector<unsigned char> once;
+        unsigned char* from;
+        if (b->sets++ == 0) {   // a batch that is set only once does without pinned memory, whose allocation takes a millisecond: this copy waits for the stream
+            once.resize(b->at.bytes);
+            from = once.data();
+        } else {
+            if (int rc = cuda_result(cudaEventSynchronize(b->uploaded), "batch_set")) return rc;   // the last upload has left the staging buffer
+            if (int rc = grow(&b->staged, &b->staged_bytes, b->at.bytes, true)) return rc;
+            from = b->staged;
+        }
+        b->at.write(b->plan, from);
+        if (int rc = cuda_result(cudaMemcpyAsync(b->data, from, b->at.bytes, cudaMemcpyHostToDevice, stream), "batch_set: upload")) return rc;
         if (int rc = cuda_result(cudaEventRecord(b->uploaded, stream), "batch_set")) return rc;
         b->set = true;
         return HTTM_OK;
@@ -255,7 +281,7 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
     a.q_head = q.stride_head, a.q_token = q.stride_token, a.out_head = out.stride_head, a.out_token = out.stride_token;
     a.k_page = k_pages.stride_page, a.k_head = k_pages.stride_head, a.k_slot = k_pages.stride_slot;
     a.v_page = v_pages.stride_page, a.v_head = v_pages.stride_head, a.v_slot = v_pages.stride_slot;
-    a.partial = b->partial;
+    a.partial = b->partial();
     a.scale_log2 = (float)(scale * 1.4426950408889634);
     a.group = c.heads / c.kv_heads;
     a.kv_heads = c.kv_heads;

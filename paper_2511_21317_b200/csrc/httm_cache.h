@@ -29,6 +29,17 @@ struct OnDevice {   // the calling thread's current device for as long as it liv
     }
 };
 
+// A stream of its own for what a handle sets up at its creation: work of the caller that is under way is not waited for.
+struct SetupStream {
+    cudaStream_t stream = nullptr;
+    cudaError_t error;
+    SetupStream() { error = cudaStreamCreateWithFlags(&stream, cudaStreamNonBlocking); }
+    cudaError_t finish() { return error == cudaSuccess ? cudaStreamSynchronize(stream) : error; }
+    ~SetupStream() {
+        if (stream) cudaStreamDestroy(stream);
+    }
+};
+
 // ---------------------------------------------------------------- rows: norms, rotation, append
 struct RowsTensor {
     const void* in;

@@ -515,11 +515,12 @@ bool rows_conflict(const httm_tensor& x, int64_t x_heads, const httm_tensor& y, 
 
 using namespace httm;
 
-constexpr int kPartialHeads = 8192;   // q's and k's together: the gradients' partial sums have their place from the start
+constexpr int kPartialHeads = 1024;   // q's and k's together: the gradients' partial sums have their place from the start
 
 struct httm_rotary {
     httm_rotary_config cfg{};
     int32_t sm_count = 148;
+    unsigned char* block = nullptr;   // of device memory; the others point into it
     float2* table = nullptr;
     float* partial = nullptr;
     int32_t* words = nullptr;   // status, arrivals of the gradients' sums [2]
@@ -527,8 +528,7 @@ struct httm_rotary {
         return RotationTable{table, cfg.n_positions, cfg.axes, cfg.rotated_dim / cfg.axes / 2, cfg.rotated_dim, cfg.interleaved};
     }
     ~httm_rotary() {
-        for (void* p : {(void*)table, (void*)partial, (void*)words})
-            if (p) cudaFree(p);
+        if (block) cudaFree(block);
     }
 };
 
@@ -608,22 +608,27 @@ int httm_rotary_create(const httm_rotary_config* config, httm_rotary** out) {
         r->cfg = c;
         r->cfg.frequencies = nullptr;
         cudaDeviceGetAttribute(&r->sm_count, cudaDevAttrMultiProcessorCount, c.device);
-        double* d_f = nullptr;
-        const int64_t n = (int64_t)(half > 0 ? c.n_positions : 0) * half;
-        int rc = alloc(&r->words, 4, "rotary");
-        if (!rc) rc = alloc(&r->partial, rows_grad_partial_floats(c.head_dim, rows_grad_chunks(kPartialHeads) + 1, r->sm_count), "rotary");
-        if (!rc && n > 0) rc = alloc(&r->table, (size_t)n, "rotary");
-        if (!rc) rc = cuda_result(cudaMemset(r->words, 0, 4 * sizeof(int32_t)), "rotary");
-        if (!rc && n > 0) {
-            rc = alloc(&d_f, (size_t)half, "rotary");
-            if (!rc) rc = cuda_result(cudaMemcpy(d_f, f.data(), half * sizeof(double), cudaMemcpyHostToDevice), "rotary");
-            if (!rc) {
-                table_kernel<<<(unsigned)((n + 255) / 256), 256>>>(r->table, d_f, n, half);
-                rc = cuda_result(cudaGetLastError(), "rotary table");
+        // one block: status and arrivals, the gradients' partial sums, the frequencies, the table
+        const size_t n = (size_t)(half > 0 ? c.n_positions : 0) * half;
+        const size_t partial_at = 256, f_at = partial_at + rows_grad_partial_floats(c.head_dim, rows_grad_chunks(kPartialHeads) + 1, r->sm_count) * sizeof(float),
+                     table_at = (f_at + half * sizeof(double) + 255) & ~(size_t)255;
+        int rc = alloc(&r->block, table_at + n * sizeof(float2), "rotary");
+        if (!rc) {
+            r->words = reinterpret_cast<int32_t*>(r->block);
+            r->partial = reinterpret_cast<float*>(r->block + partial_at);
+            r->table = reinterpret_cast<float2*>(r->block + table_at);
+            double* d_f = reinterpret_cast<double*>(r->block + f_at);
+            SetupStream setup;
+            cudaError_t e = setup.error;
+            if (e == cudaSuccess) e = cudaMemsetAsync(r->words, 0, 4 * sizeof(int32_t), setup.stream);
+            if (e == cudaSuccess && n > 0) e = cudaMemcpyAsync(d_f, f.data(), half * sizeof(double), cudaMemcpyHostToDevice, setup.stream);
+            if (e == cudaSuccess && n > 0) {
+                table_kernel<<<(unsigned)((n + 255) / 256), 256, 0, setup.stream>>>(r->table, d_f, (int64_t)n, half);
+                e = cudaGetLastError();
             }
+            if (e == cudaSuccess) e = setup.finish();
+            rc = cuda_result(e, "rotary");
         }
-        if (!rc) rc = cuda_result(cudaDeviceSynchronize(), "rotary");
-        if (d_f) cudaFree(d_f);
         if (rc) {
             delete r;
             return rc;
