@@ -6,6 +6,7 @@
 // run of its key tiles.  Jobs are dealt so that every CTA has the same number of key tiles to walk: whole row tiles as long as they fit, in order,
 // each to the CTA that has least so far (CTAs at work at the same time then read neighbouring keys), and what is left is cut where
 // a CTA is full.  A row whose keys were cut, or lie in two row tiles, leaves partial results that a last kernel adds up; others are written by their job.
+// Jobs of the narrow and of the wide kernel share the SMs out or use them in turn, see kSplitNs.
 #include <algorithm>
 #include <cmath>
 #include <exception>

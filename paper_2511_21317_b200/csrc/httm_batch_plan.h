@@ -84,6 +84,19 @@ inline int narrow_tile(int64_t tokens, int group) {
 // channels, 64 rows 53 us narrow and 44 wide).
 constexpr int kPrefixRows = 32;
 
+// What a key tile takes one SM, in ns (measured: the wide kernel's tile of 128 rows, the narrow one's tiles on the CTAs of an SM together), and what a job takes
+// beside them, in key tiles.
+constexpr double wide_tile_ns(int head_dim) { return head_dim == 64 ? 700 : 1000; }
+constexpr double narrow_tile_ns(int head_dim, int rows) { return (rows == 16 ? 680 : rows == 32 ? 900 : 1300) * (head_dim == 64 ? 0.5 : 1.0); }
+constexpr int kWideJobTiles = 6, kNarrowJobTiles = 2;
+
+// A step that needs both kernels gives each its own SMs, as many as it has work, so that they start together and an SM sees one start and one end: 32 tokens behind
+// 32 801 shared and up to 2 000 own keys of 8 heads x 128 channels 55 -> 47 us, 24 drafts of 5 tokens behind 4 001 32 -> 28, 256 sequences behind 2 000
+// 136 -> 124.  Where the wide kernel alone has more than kSplitNs to do, the narrow one goes to the SMs as they become free instead: its jobs fill
+// the wide kernel's uneven end, and an SM too many or too few for either costs more than a start (wide work of 83 us: 106 us both ways, of 131 us 176 us in turn
+// and 205 side by side).
+constexpr double kSplitNs = 64e3;
+
 // What is to be dealt: a row tile (or a pair of them) and a key head, `tiles` key tiles.
 struct BatchItem {
     int32_t seg, head, pair, tiles;
@@ -312,9 +325,19 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     Dealer d;
     d.p = p;
     d.kv_heads = c.kv_heads;
-    d.deal(wide, sole, sm_count, 6, 2);
+    int wide_sms = sm_count, narrow_sms = sm_count;
+    if (!wide.empty() && !narrow.empty() && sm_count > 1) {
+        double wide_ns = 0, narrow_ns = 0;
+        for (const BatchItem& it : wide) wide_ns += (it.tiles * it.cost + kWideJobTiles) * wide_tile_ns(c.head_dim);
+        for (const BatchItem& it : narrow) narrow_ns += (it.tiles + kNarrowJobTiles) * narrow_tile_ns(c.head_dim, p->segs[it.seg].tile_rows);
+        if (wide_ns <= kSplitNs * sm_count) {
+            wide_sms = std::min(sm_count - 1, std::max(1, (int)std::lround(sm_count * wide_ns / (wide_ns + narrow_ns))));
+            narrow_sms = sm_count - wide_sms;
+        }
+    }
+    d.deal(wide, sole, wide_sms, kWideJobTiles, 2);
     d.collect(&p->wide_jobs, &p->wide_start);
-    d.deal(narrow, sole, narrow_ctas_per_sm(c.head_dim) * sm_count, 2, 2);
+    d.deal(narrow, sole, narrow_ctas_per_sm(c.head_dim) * narrow_sms, kNarrowJobTiles, 2);
     d.collect(&p->narrow_jobs, &p->narrow_start);
     // rows whose keys were cut or lie in two row tiles; rows that see no key (they get zeros).  Two rows to a task instead of eight where they have many parts and
     // such tasks are all resident at once (4 tokens behind 32 768 keys of 8 heads x 128 channels, 32 heads 35.6 -> 34.4 us; 32 tokens, four rounds of them, 55 -> 61).
