@@ -61,7 +61,7 @@ def build_calls(force: bool = False) -> str:
     tmp = CALLS + f".{os.getpid()}.tmp"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-I", INCLUDE, "-isystem", os.path.join(root, "include"),
            "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
-           "-isystem", "/usr/local/cuda/include", src, "-o", tmp, "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_python", "-ltorch_cpu", "-ltorch"]
+           "-isystem", "/usr/local/cuda/include", src, "-o", tmp, "-L", os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-ltorch"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)

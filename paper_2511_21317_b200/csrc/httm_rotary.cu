@@ -386,10 +386,16 @@ __global__ void __launch_bounds__(kThreads, 2) rows_grad_kernel(const __grid_con
     constexpr int QUADS = 2 * D / 4, PARTS = kThreads / QUADS;
     const int quad = threadIdx.x % QUADS, part = threadIdx.x / QUADS;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 16
-    for (int c = part; c < t.ctas; c += PARTS) {
-        const float4 u = __ldcg(reinterpret_cast<const float4*>(all + (int64_t)c * 2 * D) + quad);
-        v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+    constexpr int AHEAD = 20;   // sums that a thread asks for at once; an unrolled loop's rest took a trip to L2 for each (1 044 tokens 11.6 us, so 7.8)
+    for (int c0 = part; c0 < t.ctas; c0 += PARTS * AHEAD) {
+        float4 u[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int c = c0 + i * PARTS;
+            u[i] = c < t.ctas ? __ldcg(reinterpret_cast<const float4*>(all + (int64_t)c * 2 * D) + quad) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) v.x += u[i].x, v.y += u[i].y, v.z += u[i].z, v.w += u[i].w;
     }
     float4* flat = reinterpret_cast<float4*>(smem);
     flat[threadIdx.x] = v;   // (`sums` has been read by all threads)

@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -79,6 +80,14 @@ const int32_t* positions_of(const at::Tensor* t, int64_t tokens, int64_t axes, i
     if (!lives(*t, at::kInt, device) || !shape || !t->is_contiguous())
         bad("positions: expected a contiguous int32 tensor [" + std::to_string(tokens) + "][" + std::to_string(axes) + "]" + where(device));
     return static_cast<const int32_t*>(t->data_ptr());
+}
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType dtype, int64_t device) {   // at::empty without torch's dispatcher (gradients' six tensors 10.6 -> 9.2 us)
+    return at::Tensor(at::detail::empty_cuda(sizes, dtype, at::Device(at::kCUDA, (c10::DeviceIndex)device), std::nullopt));
+}
+at::Tensor vector_of(const at::Tensor& all, int64_t i, int64_t dim) {   // the i-th of several vectors with one allocation between them
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
+    t.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef(&dim, 1), {1}, i * dim);
+    return t;
 }
 void* stream_of(PyObject* o, int64_t device) {   // an address, or None: the current stream
     if (o != Py_None) return reinterpret_cast<void*>(integer(o));
@@ -155,7 +164,7 @@ PyObject* norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
             r[i].x = rows(*x[i], names[i][0], heads, f.tokens, dim, f.dtype, device);
             const at::Tensor* out = tensor(a[12 + i], names[i][1]);
             if (!out) {
-                made[i] = at::empty({heads, f.tokens, dim}, x[i]->options());
+                made[i] = fresh({heads, f.tokens, dim}, f.dtype, device);
                 out = &made[i];
             }
             r[i].y = rows(*out, names[i][1], heads, f.tokens, dim, f.dtype, device);
@@ -184,7 +193,10 @@ PyObject* norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const First f = first_of(x[0], x[1]);
         static const char* names[2][5] = {{"q", "dq", "out_q", "q_weight", "q_bias"}, {"k", "dk", "out_k", "k_weight", "k_bias"}};
         httm_rows_grad r[2];
-        at::Tensor made[2], sums[2][2];
+        at::Tensor made[2], sums[2][2], all_sums;
+        int n_sums = 0, used = 0;
+        for (int i = 10; i < 14; ++i) n_sums += a[i] != Py_None;
+        if (n_sums > 0) all_sums = fresh({n_sums * dim}, at::kFloat, device);
         for (int i = 0; i < 2; ++i) {
             if (!x[i]) continue;
             if (!dy[i]) bad(std::string(names[i][1]) + " is missing");
@@ -193,7 +205,7 @@ PyObject* norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
             r[i].dy = rows(*dy[i], names[i][1], heads, f.tokens, dim, f.dtype, device);
             const at::Tensor* out = tensor(a[14 + i], names[i][2]);
             if (!out) {
-                made[i] = at::empty({heads, f.tokens, dim}, x[i]->options());
+                made[i] = fresh({heads, f.tokens, dim}, f.dtype, device);
                 out = &made[i];
             }
             r[i].dx = rows(*out, names[i][2], heads, f.tokens, dim, f.dtype, device);
@@ -201,8 +213,8 @@ PyObject* norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
             const at::Tensor *w = tensor(a[10 + i], names[i][3]), *b = tensor(a[12 + i], names[i][4]);
             r[i].weight = vec(w, names[i][3], dim, device);
             vec(b, names[i][4], dim, device);
-            if (w) sums[i][0] = at::empty({dim}, w->options());
-            if (b) sums[i][1] = at::empty({dim}, b->options());
+            if (w) sums[i][0] = vector_of(all_sums, used++, dim);
+            if (b) sums[i][1] = vector_of(all_sums, used++, dim);
             r[i].dweight = w ? static_cast<float*>(sums[i][0].data_ptr()) : nullptr;
             r[i].dbias = b ? static_cast<float*>(sums[i][1].data_ptr()) : nullptr;
         }
@@ -252,7 +264,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const httm_tensor tq = rows(*q, "q", heads, tokens, dim, type_of(kind), device);
         at::Tensor made;
         if (!out) {
-            made = at::empty({tokens, heads * dim}, q->options());
+            made = fresh({tokens, heads * dim}, q->scalar_type(), device);
             out = &made;
         }
         if (!lives(*out, type_of(kind), device)) bad("out: expected a CUDA tensor of q's type");
