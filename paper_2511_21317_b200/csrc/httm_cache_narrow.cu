@@ -62,11 +62,10 @@ __device__ __forceinline__ uint32_t tile_at(int row, int piece) {
 
 // The CTA's jobs are one stream of key tiles: tiles of the next job are on their way while the last ones of a job are worked on.  Up to kRecords jobs at a time lie in
 // shared memory (a CTA that has more starts over with the next ones).  The page numbers of a tile are read one tile before its copies are issued.
-constexpr int kRecords = 16, kMergeChannels = 32;
+constexpr int kRecords = 16;
 template <int D>
 struct Shared {
     unsigned char stages[kStages][kStageBytes<D>];
-    float merge[4][16][kMergeChannels + 4];   // [warp][row]; the pitch keeps rows on distinct banks
     float2 stats[4][16];
     CacheJob jobs[kRecords];
 };
@@ -149,31 +148,46 @@ struct Stream {
     }
 };
 
-// One job with a tile of 16 MT rows.  Warp w has rows 16 (w mod MT) .. and of every key tile the keys 16 MT (w / MT) .. .
-template <typename T, int D, int MT>
-__device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheJob job, Shared<D>& sm, Stream<T, D>& stream) {
-    constexpr int KG = 4 / MT, NB = 2 * MT;   // warps that share a row by keys; blocks of eight keys of a warp
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int row0 = (warp % MT) * 16 + (lane >> 2), key_base = (warp / MT) * 16 * MT;
-    const int n_rows = job.tokens[0] * a.group;
-
-    // rows as operands of the matrix instruction: this thread has rows row0 and row0 + 8
-    uint32_t qf[D / 16][4];
+// A job's rows as operands of the matrix instruction: the thread has two of them, eight apart.
+template <typename T, int D>
+struct QueryRows {
+    uint32_t of[D / 16][4];
     int seen[2];   // own keys that the two rows see
+    __device__ __forceinline__ void load(const CacheArgs& a, const CacheJob& job) {
+        const int lane = threadIdx.x & 31, row0 = (((int)threadIdx.x >> 5) & (job.tile_rows / 16 - 1)) * 16 + (lane >> 2), n_rows = job.tokens[0] * a.group;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int row = row0 + 8 * r;
-        const bool valid = row < n_rows;
-        const int token = valid ? row / a.group : 0;
-        seen[r] = min(job.own_keys[0], job.seen0[0] + (a.causal ? token : 0));
-        const T* q = static_cast<const T*>(a.q) + (int64_t)(job.token0 + token) * a.q_token + (int64_t)(job.head * a.group + (valid ? row % a.group : 0)) * a.q_head +
-                     2 * (lane & 3);
+        for (int r = 0; r < 2; ++r) {
+            const int row = row0 + 8 * r;
+            const bool valid = row < n_rows;
+            const int token = valid ? row / a.group : 0;
+            seen[r] = min(job.own_keys[0], job.seen0[0] + (a.causal ? token : 0));
+            const T* q = static_cast<const T*>(a.q) + (int64_t)(job.token0 + token) * a.q_token +
+                         (int64_t)(job.head * a.group + (valid ? row - token * a.group : 0)) * a.q_head + 2 * (lane & 3);
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-            qf[c][r] = valid ? ld_l2(q + 16 * c) : 0u;
-            qf[c][2 + r] = valid ? ld_l2(q + 16 * c + 8) : 0u;
+            for (int c = 0; c < D / 16; ++c) {
+                of[c][r] = valid ? ld_l2(q + 16 * c) : 0u;
+                of[c][2 + r] = valid ? ld_l2(q + 16 * c + 8) : 0u;
+            }
         }
     }
+};
+// Where the sums of a job's warps meet: rows of D floats in the stage of its last key tile, [warp][row].  Pieces of 16 bytes are exchanged so that four rows'
+// writes (pairs of floats, two lanes to a piece) and eight rows' reads (a piece each) lie in distinct banks.
+template <int D>
+__device__ __forceinline__ uint32_t merge_at(int warp, int row, int piece) {
+    return (uint32_t)((warp * 16 + row) * (D * 4) + ((piece ^ (((row & 3) << 1) | ((row >> 2) & 1))) << 4));
+}
+
+// One job with a tile of 16 MT rows.  Warp w has rows 16 (w mod MT) .. and of every key tile the keys 16 MT (w / MT) .. .  `query`: the job's rows; those of
+// `next` (null: there is none) are read into it ahead of the sums between warps, or each job would begin with a trip to L2.
+template <typename T, int D, int MT>
+__device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheJob job, const CacheJob* next, Shared<D>& sm, Stream<T, D>& stream,
+                                           QueryRows<T, D>& query) {
+    constexpr int KG = 4 / MT, NB = 2 * MT;   // warps that share a row by keys; blocks of eight keys of a warp
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int key_base = (warp / MT) * 16 * MT;
+    const int n_rows = job.tokens[0] * a.group;
+    unsigned char* last_stage = nullptr;
     float o[D / 8][4];
 #pragma unroll
     for (int c = 0; c < D / 8; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
@@ -182,6 +196,7 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheJob jo
     const int n_prefix = (job.prefix_keys + kNarrowKeys - 1) / kNarrowKeys;
     for (int i = job.tile0; i < job.tile1; ++i) {
         const uint32_t ks = stream.next(), vs = ks + kNarrowKeys * D * 2;
+        last_stage = sm.stages[0] + (ks - stream.base);
         const bool own = i >= n_prefix;
         const int key0 = (own ? i - n_prefix : i) * kNarrowKeys, keys = (own ? job.own_keys[0] : job.prefix_keys) - key0;
         float s[NB][4];
@@ -193,14 +208,14 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheJob jo
             for (int b = 0; b < MT; ++b) {   // sixteen keys
                 uint32_t kf[4];
                 ldmatrix4(kf, ks + tile_at<D>(key_base + 16 * b + (lane & 7) + ((lane >> 4) << 3), 2 * c + ((lane >> 3) & 1)));
-                mma<T>(s[2 * b], qf[c], kf[0], kf[1]);
-                mma<T>(s[2 * b + 1], qf[c], kf[2], kf[3]);
+                mma<T>(s[2 * b], query.of[c], kf[0], kf[1]);
+                mma<T>(s[2 * b + 1], query.of[c], kf[2], kf[3]);
             }
         }
         float top[2] = {-INFINITY, -INFINITY};
         int limit[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) limit[r] = own ? min(keys, seen[r] - key0) : keys;
+        for (int r = 0; r < 2; ++r) limit[r] = own ? min(keys, query.seen[r] - key0) : keys;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -245,50 +260,49 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheJob jo
         }
         stream.look_ahead();
     }
+    if (next) query.load(a, *next);
     // the warps that share rows, added up in the order of their keys
+    __syncthreads();   // (the last tile has been used: its stage is free until the next one's wait)
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
+        const int row = (lane >> 2) + 8 * r;
+        if (MT == 1 && r == 1 && n_rows <= 8) break;
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-        if ((lane & 3) == 0) sm.stats[warp][(lane >> 2) + 8 * r] = make_float2(m[r], l[r]);
+        if ((lane & 3) == 0) sm.stats[warp][row] = make_float2(m[r], l[r]);
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c)
+            *reinterpret_cast<float2*>(last_stage + merge_at<D>(warp, row, 2 * c + ((lane & 3) >> 1)) + 8 * (lane & 1)) = make_float2(o[c][2 * r], o[c][2 * r + 1]);
     }
-    constexpr int QUADS = kMergeChannels / 4;
+    __syncthreads();
+    // the result is stored row by row, parts quad by quad (see cache_combine_kernel)
+    constexpr int QUADS = D / 4;
+    const bool whole = job.part[0] < 0;
+    const int row_bits = 32 - __clz(n_rows - 1);   // parts: as many rows side by side as the job has, up to a power of two
+    for (int i = tid; i < (whole ? n_rows * QUADS : QUADS << row_bits); i += kThreads) {
+        const int row = whole ? i / QUADS : i & ((1 << row_bits) - 1), c = whole ? i % QUADS : i >> row_bits;
+        if (row >= n_rows) continue;
+        float2 st[KG];
+        float top = -INFINITY;
 #pragma unroll
-    for (int c0 = 0; c0 < D; c0 += kMergeChannels) {
-        if (c0 > 0) __syncthreads();   // (the channels before these have been read; of the job before this one: the key tiles' barriers)
+        for (int g = 0; g < KG; ++g) st[g] = sm.stats[g * MT + row / 16][row % 16], top = fmaxf(top, st[g].x);
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        float total = 0.f;
 #pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int c = 0; c < kMergeChannels / 8; ++c)
-                *reinterpret_cast<float2*>(&sm.merge[warp][(lane >> 2) + 8 * r][8 * c + 2 * (lane & 3)]) = make_float2(o[c0 / 8 + c][2 * r], o[c0 / 8 + c][2 * r + 1]);
-        __syncthreads();
-        for (int i = tid; i < 16 * MT * QUADS; i += kThreads) {
-            // the result is stored row by row, parts quad by quad (see cache_combine_kernel)
-            const int row = job.part[0] < 0 ? i / QUADS : i % (16 * MT), c = job.part[0] < 0 ? i % QUADS : i / (16 * MT);
-            if (row >= n_rows) continue;
-            float top = -INFINITY;
-#pragma unroll
-            for (int g = 0; g < KG; ++g) top = fmaxf(top, sm.stats[g * MT + row / 16][row % 16].x);
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            float total = 0.f;
-#pragma unroll
-            for (int g = 0; g < KG; ++g) {
-                const float2 st = sm.stats[g * MT + row / 16][row % 16];
-                const float f = st.x == -INFINITY ? 0.f : exp2_fast(st.x - top);
-                const float4 v = *reinterpret_cast<const float4*>(&sm.merge[g * MT + row / 16][row % 16][4 * c]);
-                sum.x = fmaf(v.x, f, sum.x), sum.y = fmaf(v.y, f, sum.y), sum.z = fmaf(v.z, f, sum.z), sum.w = fmaf(v.w, f, sum.w);
-                total = fmaf(st.y, f, total);
-            }
-            if (job.part[0] < 0) {
-                const float inv = top == -INFINITY ? 0.f : 1.f / total;
-                T* out = static_cast<T*>(a.out) + (int64_t)(job.token0 + row / a.group) * a.out_token + (int64_t)(job.head * a.group + row % a.group) * a.out_head +
-                         c0 + 4 * c;
-                *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum.x * inv, sum.y * inv), pack2<T>(sum.z * inv, sum.w * inv));
-            } else {
-                float* to = a.partial + (int64_t)job.part[0] * (kPartUnit * (D + 2));
-                __stcg(reinterpret_cast<float4*>(to) + (c0 / 4 + c) * 16 * MT + row, sum);
-                if (c0 == 0 && c == 0) __stcg(reinterpret_cast<float2*>(to + 16 * MT * D + 2 * row), make_float2(top, total));
-            }
+        for (int g = 0; g < KG; ++g) {
+            const float f = st[g].x == -INFINITY ? 0.f : exp2_fast(st[g].x - top);
+            const float4 v = *reinterpret_cast<const float4*>(last_stage + merge_at<D>(g * MT + row / 16, row % 16, c));
+            sum.x = fmaf(v.x, f, sum.x), sum.y = fmaf(v.y, f, sum.y), sum.z = fmaf(v.z, f, sum.z), sum.w = fmaf(v.w, f, sum.w);
+            total = fmaf(st[g].y, f, total);
+        }
+        if (whole) {
+            const float inv = top == -INFINITY ? 0.f : 1.f / total;
+            T* out = static_cast<T*>(a.out) + (int64_t)(job.token0 + row / a.group) * a.out_token + (int64_t)(job.head * a.group + row % a.group) * a.out_head + 4 * c;
+            *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(sum.x * inv, sum.y * inv), pack2<T>(sum.z * inv, sum.w * inv));
+        } else {
+            float* to = a.partial + (int64_t)job.part[0] * (kPartUnit * (D + 2));
+            __stcg(reinterpret_cast<float4*>(to) + c * 16 * MT + row, sum);
+            if (c == 0) __stcg(reinterpret_cast<float2*>(to + 16 * MT * D + 2 * row), make_float2(top, total));
         }
     }
 }
@@ -311,14 +325,17 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) cache_narrow_kernel
             waited = true;
         }
         stream.start();
+        QueryRows<T, D> query;
+        query.load(a, sm.jobs[0]);
         for (int j = 0; j < n; ++j) {
             const int rows = sm.jobs[j].tile_rows;
+            const CacheJob* next = j + 1 < n ? &sm.jobs[j + 1] : nullptr;
             if (rows == 16)
-                narrow_job<T, D, 1>(a, sm.jobs[j], sm, stream);
+                narrow_job<T, D, 1>(a, sm.jobs[j], next, sm, stream, query);
             else if (rows == 32)
-                narrow_job<T, D, 2>(a, sm.jobs[j], sm, stream);
+                narrow_job<T, D, 2>(a, sm.jobs[j], next, sm, stream, query);
             else
-                narrow_job<T, D, 4>(a, sm.jobs[j], sm, stream);
+                narrow_job<T, D, 4>(a, sm.jobs[j], next, sm, stream, query);
         }
         copies_wait<0>();
     }
