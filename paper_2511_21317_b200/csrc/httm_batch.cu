@@ -278,6 +278,7 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
     a.job_start = part_of<int32_t>(b, b->at.narrow_start);
     a.table = part_of<int32_t>(b, b->at.table);
     a.combine_tasks = part_of<CombineTask>(b, b->at.combine_tasks);
+    a.n_combine_tasks = (int32_t)p.combine_tasks.size(), a.combine_warps = p.combine_warps;
     a.q = q.ptr, a.k = k_pages.ptr, a.v = v_pages.ptr, a.out = out.ptr;
     a.q_head = q.stride_head, a.q_token = q.stride_token, a.out_head = out.stride_head, a.out_token = out.stride_token;
     a.k_page = k_pages.stride_page, a.k_head = k_pages.stride_head, a.k_slot = k_pages.stride_slot;
@@ -300,7 +301,7 @@ int httm_cache_attention(httm_batch* b, int32_t dtype, httm_pages k_pages, httm_
     a.early = !p.wide_jobs.empty();
     if (!rc && !p.narrow_jobs.empty()) rc = cuda_result(launch_cache_narrow(a, c.head_dim, dtype, (int)p.narrow_start.size() - 1, stream), "cache_attention launch");
     if (!rc && !p.combine_tasks.empty())
-        rc = cuda_result(launch_cache_combine(a, c.head_dim, dtype, (int)p.combine_tasks.size(), stream), "cache_attention launch");
+        rc = cuda_result(launch_cache_combine(a, c.head_dim, dtype, stream), "cache_attention launch");
     return rc;
 }
 

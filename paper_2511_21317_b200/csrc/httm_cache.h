@@ -138,6 +138,7 @@ struct CacheArgs {
     const int32_t* job_start;   // [CTAs + 1]
     const int32_t* table;       // pages of the prefix, then of every sequence
     const CombineTask* combine_tasks;
+    int32_t n_combine_tasks, combine_warps;   // warps to a task: 2, 4 or 8
     const void *q, *k, *v;
     void* out;
     int64_t q_head, q_token, out_head, out_token;
@@ -152,6 +153,6 @@ cudaError_t configure_cache_attention();
 cudaError_t launch_cache_narrow(const CacheArgs& a, int head_dim, int dtype, int ctas, cudaStream_t stream);
 cudaError_t configure_cache_wide();
 cudaError_t launch_cache_wide(const CacheArgs& a, int head_dim, int dtype, int64_t n_pages, int ctas, cudaStream_t stream);
-cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, int tasks, cudaStream_t stream);
+cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, cudaStream_t stream);
 
 }  // namespace httm

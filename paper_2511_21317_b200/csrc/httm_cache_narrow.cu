@@ -344,14 +344,15 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) cache_narrow_kernel
 
 // The partial results of rows whose keys were shared out, added up in the order of the keys: out = sum O_i 2^(m_i - m) / sum l_i 2^(m_i - m).  A part of a tile
 // of R rows is [D / 4][R] quads of channels and then [R] pairs (m, l): the thread of a row in the wide kernel writes with its neighbours whole lines (row
-// by row they were 32 half sectors per instruction, 4 600 .. 7 000 ns at the end of a job).  A CTA takes eight rows, or two (a whole sector) that have many parts; its warps take the parts in
-// turn, a lane some of the quads of one row, and the warps' sums meet in shared memory.  The time is that of trips to L2 behind one another, so values
+// by row they were 32 half sectors per instruction, 4 600 .. 7 000 ns at the end of a job).  A task has up to eight rows, or two (a whole sector) that have many parts; its eight, four or
+// two warps take the parts in turn, a lane some of the quads of one row, and the warps' sums meet in shared memory.  A task of four rows has its own code (all lanes
+// at work: 4 tokens of 16 heads 6.5 -> 6.1 us).  The time is that of trips to L2 behind one another, so values
 // are asked for together with the maxima that weight them.  A row without parts gets zeros.
-template <typename T, int D, int ROWS>
-__device__ __forceinline__ void combine_rows(const CacheArgs& a, const CombineTask& task, float (*sums)[kCombineRows][D + 4], float2 (*stats)[kCombineRows]) {
+template <typename T, int D, int ROWS, int WARPS>
+__device__ __forceinline__ void combine_rows(const CacheArgs& a, const CombineTask& task, float (*sums)[kCombineRows][D + 4], float2 (*stats)[kCombineRows], int warp) {
     constexpr int STEP = 32 / ROWS, Q = D / 4 / STEP;   // a lane has the quads q, q + STEP, ..: Q of them
     constexpr int BATCH = Q < 2 ? 4 : 8 / Q;            // parts that it asks for at a time (twice as many: 7.4 instead of 7.0 us for 4 tokens)
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane % ROWS, quad = lane / ROWS;
+    const int lane = threadIdx.x & 31, row = lane % ROWS, quad = lane / ROWS;
     const int n0 = task.parts[0], n = n0 + task.parts[1];   // those of the prefix come first
     const float* base[2];
     int64_t stride[2];
@@ -365,12 +366,12 @@ __device__ __forceinline__ void combine_rows(const CacheArgs& a, const CombineTa
 #pragma unroll
     for (int c = 0; c < Q; ++c) sum[c] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (row < task.rows) {
-        for (int p0 = warp; p0 < n; p0 += BATCH * kCombineWarps) {
+        for (int p0 = warp; p0 < n; p0 += BATCH * WARPS) {
             float2 st[BATCH];
             float4 v[BATCH][Q];
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
-                const int p = p0 + i * kCombineWarps;
+                const int p = p0 + i * WARPS;
                 st[i] = make_float2(-INFINITY, 0.f);
 #pragma unroll
                 for (int c = 0; c < Q; ++c) v[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -407,9 +408,30 @@ __device__ __forceinline__ void combine_rows(const CacheArgs& a, const CombineTa
             if (quad == 0) stats[warp][row] = make_float2(top, total);
         }
     }
+}
+
+template <typename T, int D, int WARPS>
+__global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const __grid_constant__ CacheArgs a) {
+    __shared__ __align__(16) float all_sums[kCombineWarps][kCombineRows][D + 4];
+    __shared__ float2 all_stats[kCombineWarps][kCombineRows];
+    // warps first .. first + WARPS - 1 have a task together
+    const int first = WARPS == kCombineWarps ? 0 : (int)(threadIdx.x >> 5) & ~(WARPS - 1), warp = (int)(threadIdx.x >> 5) - first;
+    const int at_task = (int)blockIdx.x * (kCombineWarps / WARPS) + first / WARPS;
+    CombineTask task{};
+    if (WARPS == kCombineWarps || at_task < a.n_combine_tasks) task = ld_record(a.combine_tasks + at_task);
+    depend_wait();
+    dependents_launch();
+    auto sums = all_sums + first;
+    auto stats = all_stats + first;
+    if (task.room == kCombineFewRows)
+        combine_rows<T, D, kCombineFewRows, WARPS>(a, task, sums, stats, warp);
+    else if (task.rows <= kCombineRows / 2)
+        combine_rows<T, D, kCombineRows / 2, WARPS>(a, task, sums, stats, warp);
+    else
+        combine_rows<T, D, kCombineRows, WARPS>(a, task, sums, stats, warp);
     __syncthreads();
-    const int warps = min(n, kCombineWarps);
-    for (int i = threadIdx.x; i < task.rows * (D / 4); i += 32 * kCombineWarps) {
+    const int warps = min(task.parts[0] + task.parts[1], WARPS);
+    for (int i = (int)threadIdx.x - 32 * first; i < task.rows * (D / 4); i += 32 * WARPS) {
         const int r = i / (D / 4), c = i % (D / 4);
         float high = -INFINITY, l = 0.f;
         for (int w = 0; w < warps; ++w) high = fmaxf(high, stats[w][r].x);
@@ -428,19 +450,6 @@ __device__ __forceinline__ void combine_rows(const CacheArgs& a, const CombineTa
     }
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(32 * kCombineWarps) cache_combine_kernel(const __grid_constant__ CacheArgs a) {
-    __shared__ __align__(16) float sums[kCombineWarps][kCombineRows][D + 4];
-    __shared__ float2 stats[kCombineWarps][kCombineRows];
-    const CombineTask task = ld_record(a.combine_tasks + blockIdx.x);
-    depend_wait();
-    dependents_launch();
-    if (task.room == kCombineRows)
-        combine_rows<T, D, kCombineRows>(a, task, sums, stats);
-    else
-        combine_rows<T, D, kCombineFewRows>(a, task, sums, stats);
-}
-
 template <typename F>
 cudaError_t allow_smem(F kernel, int bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -450,8 +459,11 @@ cudaError_t narrow_of(const CacheArgs& a, int ctas, cudaStream_t stream) {
     return launch_kernel(cache_narrow_kernel<T, D>, ctas, kThreads, sizeof(Shared<D>), stream, a);
 }
 template <typename T, int D>
-cudaError_t combine_of(const CacheArgs& a, int tasks, cudaStream_t stream) {
-    return launch_kernel(cache_combine_kernel<T, D>, tasks, 32 * kCombineWarps, 0, stream, a);
+cudaError_t combine_of(const CacheArgs& a, cudaStream_t stream) {
+    const int at_once = kCombineWarps / a.combine_warps, ctas = (a.n_combine_tasks + at_once - 1) / at_once;
+    if (a.combine_warps == 8) return launch_kernel(cache_combine_kernel<T, D, 8>, ctas, 32 * kCombineWarps, 0, stream, a);
+    if (a.combine_warps == 4) return launch_kernel(cache_combine_kernel<T, D, 4>, ctas, 32 * kCombineWarps, 0, stream, a);
+    return launch_kernel(cache_combine_kernel<T, D, 2>, ctas, 32 * kCombineWarps, 0, stream, a);
 }
 
 }  // namespace
@@ -468,9 +480,9 @@ cudaError_t launch_cache_narrow(const CacheArgs& a, int head_dim, int dtype, int
     if (dtype == HTTM_BF16) return head_dim == 64 ? narrow_of<__nv_bfloat16, 64>(a, ctas, stream) : narrow_of<__nv_bfloat16, 128>(a, ctas, stream);
     return head_dim == 64 ? narrow_of<__half, 64>(a, ctas, stream) : narrow_of<__half, 128>(a, ctas, stream);
 }
-cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, int tasks, cudaStream_t stream) {
-    if (dtype == HTTM_BF16) return head_dim == 64 ? combine_of<__nv_bfloat16, 64>(a, tasks, stream) : combine_of<__nv_bfloat16, 128>(a, tasks, stream);
-    return head_dim == 64 ? combine_of<__half, 64>(a, tasks, stream) : combine_of<__half, 128>(a, tasks, stream);
+cudaError_t launch_cache_combine(const CacheArgs& a, int head_dim, int dtype, cudaStream_t stream) {
+    if (dtype == HTTM_BF16) return head_dim == 64 ? combine_of<__nv_bfloat16, 64>(a, stream) : combine_of<__nv_bfloat16, 128>(a, stream);
+    return head_dim == 64 ? combine_of<__half, 64>(a, stream) : combine_of<__half, 128>(a, stream);
 }
 
 }  // namespace httm
