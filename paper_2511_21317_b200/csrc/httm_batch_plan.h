@@ -86,10 +86,12 @@ inline int narrow_tile(int64_t tokens, int group) {
 constexpr int kPrefixRows = 32;
 
 // What a key tile takes one SM, in ns (measured: the wide kernel's tile of 128 rows, the narrow one's tiles on the CTAs of an SM together), and what a job takes
-// beside them, in key tiles.
+// beside them, in key tiles (as its CTA is dealt them: a job that is cut needs its sum too; a narrow one alone takes 1.3).
 constexpr double wide_tile_ns(int head_dim) { return head_dim == 64 ? 700 : 1000; }
-constexpr double narrow_tile_ns(int head_dim, int rows) { return (rows == 16 ? 680 : rows == 32 ? 900 : 1300) * (head_dim == 64 ? 0.5 : 1.0); }
+constexpr double narrow_tile_ns(int head_dim, int rows) { return (rows == 16 ? 780 : rows == 32 ? 900 : 1300) * (head_dim == 64 ? 0.5 : 1.0); }
 constexpr int kWideJobTiles = 6, kNarrowJobTiles = 2;
+constexpr double kNarrowOneJob = 1.3;
+constexpr double kWideStartNs = 2000;   // by so much the wide kernel's start and end take longer
 
 // A step that needs both kernels gives each its own SMs, as many as it has work, so that they start together and an SM sees one start and one end: 32 tokens behind
 // 32 801 shared and up to 2 000 own keys of 8 heads x 128 channels 55 -> 47 us, 24 drafts of 5 tokens behind 4 001 32 -> 28, 256 sequences behind 2 000
@@ -330,9 +332,13 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     if (!wide.empty() && !narrow.empty() && sm_count > 1) {
         double wide_ns = 0, narrow_ns = 0;
         for (const BatchItem& it : wide) wide_ns += (it.tiles * it.cost + kWideJobTiles) * wide_tile_ns(c.head_dim);
-        for (const BatchItem& it : narrow) narrow_ns += (it.tiles + kNarrowJobTiles) * narrow_tile_ns(c.head_dim, p->segs[it.seg].tile_rows);
+        for (const BatchItem& it : narrow) narrow_ns += (it.tiles + kNarrowOneJob) * narrow_tile_ns(c.head_dim, p->segs[it.seg].tile_rows);
         if (wide_ns <= kSplitNs * sm_count) {
-            wide_sms = std::min(sm_count - 1, std::max(1, (int)std::lround(sm_count * wide_ns / (wide_ns + narrow_ns))));
+            double least = 0;
+            for (int w = 1; w < sm_count; ++w) {
+                const double t = std::max(kWideStartNs + wide_ns / w, narrow_ns / (sm_count - w));
+                if (w == 1 || t < least) least = t, wide_sms = w;
+            }
             narrow_sms = sm_count - wide_sms;
         }
     }
