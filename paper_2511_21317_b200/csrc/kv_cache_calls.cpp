@@ -1,8 +1,9 @@
 // The calls of the operators around a kept scene from Python: checks of the tensors, marshalling, and the call of the C ABI, in one step.
 //
 // A call on a few tokens takes the GPU 2 - 7 us; attribute by attribute in Python its nine tensors cost more than that (host time of norm_rotate
-// on one token with ctypes 11.4 us, with this 4.9; of its gradients 24 and 10.4, of append 9.4 and 5.1, of an attention of two kernels 12.8 and 8.3).  The functions get a handle, the sizes that the Python object keeps, and tensors or None; they raise
-// HttmError with the library's codes.  Nothing is kept from call to call.
+// on one token with ctypes 11.4 us, with this 4.5; of its gradients 24 and 7.5, of append 9.4 and 4.7, of an attention of two kernels 12.8 and 6.8).
+// The functions get a handle, the sizes that the Python object keeps, and tensors or None; they raise HttmError with the library's codes.  Nothing is kept
+// from call to call.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
