@@ -404,3 +404,27 @@ def test_refusals():
         b.set(T, L, [[1], [2]], P, 64)
     b.close()
     refuses(-1, sc.cache.attention, b, sc.q)
+
+
+STEPS = {
+    "more jobs than a CTA reads at once": ([1 + i % 3 for i in range(700)], [1] * 700, 0, 32, 8, 128, 16, {}),
+    "two kernels, few parts to a row": ([1 + i % 70 for i in range(300)], [1] * 300, 130, 32, 8, 128, 16, {}),
+    "two kernels, one row to a task, fp16": ([1 + i % 40 for i in range(300)], [1] * 300, 100, 16, 16, 64, 64, dict(dtype=torch.float16)),
+    "two kernels, tiles of 16, 32 and 64 rows": ([20 + 7 * i for i in range(64)], [(1, 8, 16, 4)[i % 4] for i in range(64)], 5000, 32, 8, 128, 32, {}),
+    "two kernels, one row tile, long prefix": ([1 + i for i in range(32)], [1] * 32, 9000, 16, 4, 64, 64, {}),
+    "much for the wide kernel, tokens beside it": ([300 + i for i in range(30)] + [40] * 20, [300] * 30 + [2] * 20, 2000, 32, 8, 128, 64, {}),
+}
+
+
+@pytest.mark.parametrize("name", STEPS)
+def test_steps_of_many_sequences(name):
+    """Both kernels side by side and one behind the other; jobs of different heights one after the other in a CTA; every way to add parts up."""
+    *a, kw = STEPS[name]
+    sc = Scene(*a, **kw, seed=len(name))
+    for _ in range(3):   # (the same workspace again, nothing waited for)
+        out = torch.full((sum(sc.queries), sc.heads * sc.dim), float("nan"), dtype=sc.dtype, device=DEV)
+        sc.cache.attention(sc.batch, sc.q, out)
+    first = sc.cache.attention(sc.batch, sc.q)
+    assert sc.batch.status() == 0
+    assert torch.equal(first, out)
+    sc.check(out, what=name)
