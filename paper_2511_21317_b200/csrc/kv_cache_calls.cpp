@@ -9,6 +9,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -82,18 +83,29 @@ const int32_t* positions_of(const at::Tensor* t, int64_t tokens, int64_t axes, i
         bad("positions: expected a contiguous int32 tensor [" + std::to_string(tokens) + "][" + std::to_string(axes) + "]" + where(device));
     return static_cast<const int32_t*>(t->data_ptr());
 }
-at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType dtype, int64_t device) {   // at::empty without torch's dispatcher (gradients' six tensors 10.6 -> 9.2 us)
-    return at::Tensor(at::detail::empty_cuda(sizes, dtype, at::Device(at::kCUDA, (c10::DeviceIndex)device), std::nullopt));
-}
 at::Tensor vector_of(const at::Tensor& all, int64_t i, int64_t dim) {   // the i-th of several vectors with one allocation between them
     at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
     t.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef(&dim, 1), {1}, i * dim);
     return t;
 }
-void* stream_of(PyObject* o, int64_t device) {   // an address, or None: the current stream
-    if (o != Py_None) return reinterpret_cast<void*>(integer(o));
-    return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
-}
+// The stream of a call: an address, or None for the current one.  New tensors belong to it, whatever the current stream has still to do with the memory they get.
+struct Stream {
+    void* at;
+    int64_t device;
+    c10::cuda::OptionalCUDAStreamGuard guard;
+    Stream(PyObject* o, int64_t device_) : device(device_) {
+        if (o == Py_None) {
+            at = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
+        } else {
+            at = reinterpret_cast<void*>(integer(o));
+            guard.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(at), (c10::DeviceIndex)device));
+        }
+    }
+    // at::empty without torch's dispatcher (gradients' six tensors 10.6 -> 9.2 us)
+    at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType dtype) const {
+        return at::Tensor(at::detail::empty_cuda(sizes, dtype, at::Device(at::kCUDA, (c10::DeviceIndex)device), std::nullopt));
+    }
+};
 PyObject* wrap(const at::Tensor* t, PyObject* given) {   // the tensor that was given, or a new one; None
     if (given && given != Py_None) return Py_NewRef(given);
     return t ? THPVariable_Wrap(*t) : Py_NewRef(Py_None);
@@ -154,6 +166,7 @@ PyObject* norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         httm_rotary* h = handle<httm_rotary>(a[0]);
         const int64_t dim = integer(a[1]), axes = integer(a[2]), rotated = integer(a[3]), device = integer(a[4]);
+        const Stream stream(a[14], device);
         const at::Tensor* x[2] = {tensor(a[5], "q"), tensor(a[6], "k")};
         const First f = first_of(x[0], x[1]);
         static const char* names[2][4] = {{"q", "out_q", "q_weight", "q_bias"}, {"k", "out_k", "k_weight", "k_bias"}};
@@ -165,7 +178,7 @@ PyObject* norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
             r[i].x = rows(*x[i], names[i][0], heads, f.tokens, dim, f.dtype, device);
             const at::Tensor* out = tensor(a[12 + i], names[i][1]);
             if (!out) {
-                made[i] = fresh({heads, f.tokens, dim}, f.dtype, device);
+                made[i] = stream.fresh({heads, f.tokens, dim}, f.dtype);
                 out = &made[i];
             }
             r[i].y = rows(*out, names[i][1], heads, f.tokens, dim, f.dtype, device);
@@ -176,7 +189,7 @@ PyObject* norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* p = rotated > 0 ? tensor(a[7], "positions") : nullptr;
         if (rotated > 0 && !p) bad("positions are missing");
         check(g_abi.norm_rotate(h, f.kind, f.tokens, positions_of(p, f.tokens, axes, device), x[0] ? &r[0] : nullptr, x[1] ? &r[1] : nullptr,
-                                stream_of(a[14], device)));
+                                stream.at));
         PyObject* out = PyTuple_New(2);
         for (int i = 0; out && i < 2; ++i) PyTuple_SET_ITEM(out, i, x[i] ? wrap(&made[i], a[12 + i]) : Py_NewRef(Py_None));
         return out;
@@ -190,6 +203,7 @@ PyObject* norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         httm_rotary* h = handle<httm_rotary>(a[0]);
         const int64_t dim = integer(a[1]), axes = integer(a[2]), rotated = integer(a[3]), device = integer(a[4]);
+        const Stream stream(a[16], device);
         const at::Tensor *dy[2] = {tensor(a[5], "dq"), tensor(a[6], "dk")}, *x[2] = {tensor(a[7], "q"), tensor(a[8], "k")};
         const First f = first_of(x[0], x[1]);
         static const char* names[2][5] = {{"q", "dq", "out_q", "q_weight", "q_bias"}, {"k", "dk", "out_k", "k_weight", "k_bias"}};
@@ -197,7 +211,7 @@ PyObject* norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor made[2], sums[2][2], all_sums;
         int n_sums = 0, used = 0;
         for (int i = 10; i < 14; ++i) n_sums += a[i] != Py_None;
-        if (n_sums > 0) all_sums = fresh({n_sums * dim}, at::kFloat, device);
+        if (n_sums > 0) all_sums = stream.fresh({n_sums * dim}, at::kFloat);
         for (int i = 0; i < 2; ++i) {
             if (!x[i]) continue;
             if (!dy[i]) bad(std::string(names[i][1]) + " is missing");
@@ -206,7 +220,7 @@ PyObject* norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
             r[i].dy = rows(*dy[i], names[i][1], heads, f.tokens, dim, f.dtype, device);
             const at::Tensor* out = tensor(a[14 + i], names[i][2]);
             if (!out) {
-                made[i] = fresh({heads, f.tokens, dim}, f.dtype, device);
+                made[i] = stream.fresh({heads, f.tokens, dim}, f.dtype);
                 out = &made[i];
             }
             r[i].dx = rows(*out, names[i][2], heads, f.tokens, dim, f.dtype, device);
@@ -222,7 +236,7 @@ PyObject* norm_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* p = rotated > 0 ? tensor(a[9], "positions") : nullptr;
         if (rotated > 0 && !p) bad("positions are missing");
         check(g_abi.norm_rotate_backward(h, f.kind, f.tokens, positions_of(p, f.tokens, axes, device), x[0] ? &r[0] : nullptr, x[1] ? &r[1] : nullptr,
-                                         stream_of(a[16], device)));
+                                         stream.at));
         PyObject* out = PyTuple_New(6);
         for (int i = 0; out && i < 2; ++i) {
             PyTuple_SET_ITEM(out, i, x[i] ? wrap(&made[i], a[14 + i]) : Py_NewRef(Py_None));
@@ -240,6 +254,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         httm_batch* b = handle<httm_batch>(a[0]);
         const int64_t heads = integer(a[1]), tokens = integer(a[2]), dim = integer(a[3]), device = integer(a[4]), kind = integer(a[5]);
+        const Stream stream(a[14], device);
         const httm_pages* pages = reinterpret_cast<const httm_pages*>(integer(a[6]));
         const at::Tensor *k = tensor(a[7], "k"), *v = tensor(a[8], "v");
         if (!k || !v) bad("k or v is missing");
@@ -248,7 +263,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* p = tensor(a[11], "positions");
         if (p && !r) bad("positions without a rotary handle");
         check(g_abi.append(b, (int32_t)kind, pages[0], pages[1], tk, tv, r, positions_of(p, tokens, integer(a[10]), device),
-                           vec(tensor(a[12], "k_weight"), "k_weight", dim, device), vec(tensor(a[13], "k_bias"), "k_bias", dim, device), stream_of(a[14], device)));
+                           vec(tensor(a[12], "k_weight"), "k_weight", dim, device), vec(tensor(a[13], "k_bias"), "k_bias", dim, device), stream.at));
         Py_RETURN_NONE;
     });
 }
@@ -259,13 +274,14 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         httm_batch* b = handle<httm_batch>(a[0]);
         const int64_t heads = integer(a[1]), tokens = integer(a[2]), dim = integer(a[3]), device = integer(a[4]), kind = integer(a[5]);
+        const Stream stream(a[10], device);
         const httm_pages* pages = reinterpret_cast<const httm_pages*>(integer(a[6]));
         const at::Tensor *q = tensor(a[7], "q"), *out = tensor(a[8], "out");
         if (!q) bad("q is missing");
         const httm_tensor tq = rows(*q, "q", heads, tokens, dim, type_of(kind), device);
         at::Tensor made;
         if (!out) {
-            made = fresh({tokens, heads * dim}, q->scalar_type(), device);
+            made = stream.fresh({tokens, heads * dim}, q->scalar_type());
             out = &made;
         }
         if (!lives(*out, type_of(kind), device)) bad("out: expected a CUDA tensor of q's type");
@@ -281,7 +297,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
             PyErr_Clear();
             bad("scale: expected a number");
         }
-        check(g_abi.attention(b, (int32_t)kind, pages[0], pages[1], tq, to, scale, stream_of(a[10], device)));
+        check(g_abi.attention(b, (int32_t)kind, pages[0], pages[1], tq, to, scale, stream.at));
         return wrap(out, a[8]);
     });
 }

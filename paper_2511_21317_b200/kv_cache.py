@@ -80,7 +80,7 @@ def _bad(message: str):
 
 
 def _address(stream):
-    """For the calls: None stands for the current stream."""
+    """For the calls: None stands for the current stream; tensors that a call makes belong to its stream."""
     return None if stream is None else stream.cuda_stream
 
 

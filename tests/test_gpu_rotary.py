@@ -366,3 +366,22 @@ def test_refusals_of_the_gradients():
     assert rot.norm_rotate_backward(q, None, q, None, pos)[1:] == (None,) * 5
     with pytest.raises(TypeError):
         rot.norm_rotate_backward(q)
+
+
+def test_outputs_made_on_another_stream_are_its_own():
+    """New tensors of a call with a stream of its own get no memory that the current stream has still to write to."""
+    n, heads, dim = 300, 8, 64
+    rotary = kc.Rotary(dim, 1024, norm="rms")
+    q = torch.randn(heads, n, dim, device=DEV).to(torch.bfloat16)
+    positions = torch.arange(n, dtype=torch.int32, device=DEV)
+    want, _ = rotary.norm_rotate(q, None, positions)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    held = [torch.empty_like(q) for _ in range(8)]   # blocks of the size that the call will ask for
+    torch.cuda._sleep(20_000_000)
+    for t in held:
+        t.fill_(7.0)
+    del held, t
+    got, _ = rotary.norm_rotate(q, None, positions, stream=other)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
