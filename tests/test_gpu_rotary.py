@@ -376,12 +376,13 @@ def test_outputs_made_on_another_stream_are_its_own():
     positions = torch.arange(n, dtype=torch.int32, device=DEV)
     want, _ = rotary.norm_rotate(q, None, positions)
     other = torch.cuda.Stream()
+    held = [torch.empty_like(q).fill_(1.0) for _ in range(12)]   # blocks of the size that the call will ask for
+    torch.cuda._sleep(1)   # (what is used below is loaded)
     torch.cuda.synchronize()
-    held = [torch.empty_like(q) for _ in range(8)]   # blocks of the size that the call will ask for
-    torch.cuda._sleep(20_000_000)
-    for t in held:
-        t.fill_(7.0)
-    del held, t
+    torch.cuda._sleep(100_000_000)
+    for i in range(1, 11):
+        held[i].fill_(7.0)
+    del held[2:10:2]   # (each between two that stay: free blocks of just that size)
     got, _ = rotary.norm_rotate(q, None, positions, stream=other)
     torch.cuda.synchronize()
     assert torch.equal(got, want)
