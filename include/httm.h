@@ -440,8 +440,9 @@ int httm_batch_status(httm_batch* batch, int64_t* status);
  *                j % page_size of page j / page_size
  *   prefix_pages, prefix_length   the keys that every sequence sees in front of its own
  * A plan of the attention is made here, so that a batch serves all layers of a step.  It is uploaded on `cuda_stream`; memory
- * grows here when a batch is larger than all before it, nothing is allocated in the calls below.  Errors: INVALID_ARG (a page
- * that does not exist, a negative length), UNSUPPORTED, NOMEM, CUDA; the batch is then empty.
+ * grows here when a batch is larger than all before it, nothing is allocated in the calls below.  A graph that captured the
+ * calls below holds this plan's places and must not be replayed behind the next one.  Errors: INVALID_ARG (a page that does not
+ * exist, a negative length), UNSUPPORTED (a stream that is being captured), NOMEM, CUDA; the batch is then empty.
  */
 int httm_batch_set(httm_batch* batch, int32_t n_sequences, const int32_t* lengths, const int32_t* queries, const int32_t* tables,
                    int64_t table_stride, const int32_t* prefix_pages, int32_t prefix_length, void* cuda_stream);

@@ -185,13 +185,16 @@ int httm_batch_set(httm_batch* b, int32_t n_sequences, const int32_t* lengths, c
         std::string why;
         const BatchInput in{n_sequences, lengths, queries, tables, table_stride, prefix_pages, prefix_length};
         if (int rc = check_batch(b->cfg, in, &why)) return global_fail(rc, "batch_set: %s", why.c_str());
-        make_batch_plan(b->cfg, in, b->sm_count, &b->plan);
         OnDevice guard(b->cfg.device);
         if (!guard.ok) return global_fail(HTTM_ERR_CUDA, "batch_set: cudaSetDevice failed");
+        cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        if (int rc = cuda_result(cudaStreamIsCapturing(stream, &capture), "batch_set")) return rc;
+        if (capture != cudaStreamCaptureStatusNone) return global_fail(HTTM_ERR_UNSUPPORTED, "batch_set: the stream is being captured");
+        make_batch_plan(b->cfg, in, b->sm_count, &b->plan);
         b->at = BatchLayout(b->plan);
         const size_t partial_bytes = (size_t)b->plan.part_units * kPartUnit * (b->cfg.head_dim + 2) * sizeof(float);
         if (int rc = grow(&b->data, &b->data_bytes, b->at.bytes + partial_bytes, false)) return rc;
-        cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
         std::vector<unsigned char> once;
         unsigned char* from;
         if (b->sets++ == 0) {   // a batch that is set only once does without pinned memory, whose allocation takes a millisecond: this copy waits for the stream

@@ -197,7 +197,8 @@ class CacheBatch(_Handle):
 
     def set(self, tables, lengths, queries, prefix_pages=(), prefix_length: int = 0, stream=None):
         """tables: the pages of every sequence (a list of lists, or a 2-D integer array); lengths: its keys, the new ones included; queries:
-        its query tokens; all on the host.  The plan is uploaded on `stream`."""
+        its query tokens; all on the host.  The plan is uploaded on `stream`.  A CUDA graph that captured calls with this batch holds for this plan
+        alone: capture again behind the next set()."""
         self.n_tokens = 0
         n_seq = len(lengths)
         lengths, queries = (np.ascontiguousarray(x, dtype=np.int32) for x in (lengths, queries))

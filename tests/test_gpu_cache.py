@@ -428,3 +428,20 @@ def test_steps_of_many_sequences(name):
     assert sc.batch.status() == 0
     assert torch.equal(first, out)
     sc.check(out, what=name)
+
+
+def test_a_batch_is_not_set_while_its_stream_is_captured():
+    sc = Scene([40, 30], [3, 2], 64, 4, 2, 64, 16, seed=1)
+    fresh = kc.CacheBatch(4, 2, 64, 16, sc.n_pages)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for batch in (sc.batch, fresh):
+            with pytest.raises(hb.HttmError) as e:
+                batch.set(sc.tables, sc.lengths, sc.queries, sc.prefix_pages, 64)
+            assert e.value.code == -2
+        doubled = sc.q * 2   # (the capture goes on)
+    graph.replay()
+    assert torch.equal(doubled, sc.q * 2)
+    for batch in (sc.batch, fresh):
+        batch.set(sc.tables, sc.lengths, sc.queries, sc.prefix_pages, 64)
+        sc.check(sc.cache.attention(batch, sc.q))
