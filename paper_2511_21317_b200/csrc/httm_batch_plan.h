@@ -58,7 +58,7 @@ inline int check_batch(const httm_batch_config& c, const BatchInput& in, std::st
     const int32_t n_prefix = pages_of(in.prefix_length, c.page_size);
     if (n_prefix > 0 && !in.prefix_pages) return bad(HTTM_ERR_INVALID_ARG, "null array");
     if (n_prefix > 0 && !pages_exist(in.prefix_pages, n_prefix)) return bad(HTTM_ERR_INVALID_ARG, "a page of the prefix does not exist");
-    int64_t tokens = 0, pages = n_prefix;
+    int64_t tokens = 0, pages = (int64_t)n_prefix + 3;
     for (int32_t i = 0; i < in.n_sequences; ++i) {
         if (in.lengths[i] < 0 || in.queries[i] < 0) return bad(HTTM_ERR_INVALID_ARG, "a length is negative");
         const int32_t n = pages_of(in.lengths[i], c.page_size);
@@ -67,7 +67,7 @@ inline int check_batch(const httm_batch_config& c, const BatchInput& in, std::st
         if (!pages_exist(in.tables + i * in.table_stride, n)) return bad(HTTM_ERR_INVALID_ARG, "a page of a sequence does not exist");
         if ((int64_t)in.lengths[i] + in.prefix_length > (1ll << 31) - 1 - kWideKeys) return bad(HTTM_ERR_UNSUPPORTED, "more than 2^31 keys");
         tokens += in.queries[i];
-        pages += n;
+        pages += ((int64_t)n + 3) & ~(int64_t)3;
     }
     if (tokens * c.heads > (1ll << 31) - 1) return bad(HTTM_ERR_UNSUPPORTED, "tokens * heads must be below 2^31");
     if (pages > (1ll << 31) - 1) return bad(HTTM_ERR_UNSUPPORTED, "too many pages");
@@ -235,6 +235,7 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
     for (int i = 0; i < n_seq; ++i) {
         const int32_t length = in.lengths[i], nq = in.queries[i], n = pages_of(length, page);
         const int32_t* t = in.tables + i * in.table_stride;
+        p->table.resize((p->table.size() + 3) & ~(size_t)3, 0);   // (read four at a time)
         table_at[i] = (int32_t)p->table.size();
         token_at[i] = p->n_tokens;
         if (n > 0) p->table.insert(p->table.end(), t, t + n);

@@ -63,71 +63,78 @@ __device__ __forceinline__ uint32_t tile_at(int row, int piece) {
 }
 
 // The CTA's jobs are one stream of key tiles: tiles of the next job are on their way while the last ones of a job are worked on.  Up to kRecords jobs at a time lie in
-// shared memory (a CTA that has more starts over with the next ones).  The page numbers of a tile are read one tile before its copies are issued.
-constexpr int kRecords = 16;
+// shared memory (a CTA that has more starts over with the next ones).  Thread 0 goes ahead of the copies: with a tile's copies it asks for the page numbers of the one
+// that is fetched when they have arrived (four entries of the table, enough for the smallest pages; runs of pages begin at multiples of four).
+constexpr int kRecords = 16, kAheadSlots = 8;
+struct alignas(16) TileAhead {
+    int32_t head, key0, keys, pad;
+    int32_t pages[4];
+};
 template <int D>
 struct Shared {
     unsigned char stages[kStages][kStageBytes<D>];
     float2 stats[4][16];
+    TileAhead ahead[kAheadSlots];
     CacheJob jobs[kRecords];
 };
 template <typename T, int D>
 struct Stream {
     static constexpr int PIECES = D / 8, ROWS = kThreads / PIECES, COUNT = kNarrowKeys / ROWS;   // 16-byte pieces of a row; rows that the CTA copies at once
+    static constexpr int AHEAD = kStages - 1;                                                    // tiles in flight
+    static_assert(AHEAD + 2 <= kAheadSlots, "a tile's place is not written while another is read in it");
     const CacheArgs& a;
     Shared<D>& sm;
-    uint32_t base;      // of the stages
-    int n_jobs, job = -1;   // the job whose tiles are being read ahead
-    int left = 0;           // its tiles behind the one at hand
-    int own_keys, own_table;
-    int issued = 0, used = 0;
-    // the tile that is fetched next: its keys, their pages
-    int32_t pages[4];
-    const int32_t* table;
-    int head, key0, end, keys = 0;   // end: keys of the prefix / of the sequence
-    bool more;                       // own keys follow
-    __device__ __forceinline__ Stream(const CacheArgs& a_, Shared<D>& sm_, int n) : a(a_), sm(sm_), base(smem_of(sm_.stages[0])), n_jobs(n) { look_ahead(); }
-    __device__ __forceinline__ void start() {
-        for (int i = 0; i < kStages - 1; ++i) {
-            fetch();
-            look_ahead();
-        }
+    uint32_t base;          // of the stages
+    int n_jobs;
+    int issued = 0, used = 0, fetched = 0;
+    // thread 0: the job it has come to, the tile behind the last one that it has noted
+    int job = -1, left = 0, key0 = 0, end = 0;   // left: tiles of the job; end: keys of the prefix / of the sequence
+    const int32_t* table = nullptr;
+    bool more = false;                           // own keys follow
+    __device__ __forceinline__ Stream(const CacheArgs& a_, Shared<D>& sm_, int n) : a(a_), sm(sm_), base(smem_of(sm_.stages[0])), n_jobs(n) {
+        for (int i = 0; i < AHEAD; ++i) note(i);
+        copies_commit();
+        copies_wait<0>();
+        __syncthreads();
     }
-    // Called behind the work on a tile, so that the page numbers arrive while the CTA waits for its next tile.
-    __device__ __forceinline__ void look_ahead() {
-        if (left > 0) {
-            --left;
-            key0 += kNarrowKeys;
-            if (more && key0 >= end) key0 = 0, end = own_keys, table = a.table + own_table, more = false;
-        } else {
-            keys = 0;
-            if (++job >= n_jobs) return;
-            const int tile = sm.jobs[job].tile0, prefix = sm.jobs[job].prefix_keys, n_prefix = (prefix + kNarrowKeys - 1) / kNarrowKeys;
-            left = sm.jobs[job].tile1 - tile - 1;
-            head = sm.jobs[job].head;
-            own_keys = sm.jobs[job].own_keys[0], own_table = sm.jobs[job].own_table;
-            more = tile < n_prefix;
-            key0 = (more ? tile : tile - n_prefix) * kNarrowKeys;
-            end = more ? prefix : own_keys;
-            table = a.table + (more ? 0 : own_table);
+    __device__ __forceinline__ void start() {
+        for (int i = 0; i < AHEAD; ++i) fetch();
+    }
+    __device__ __forceinline__ void note(int tile) {   // the stream's tile of that number, or that there is none
+        if (threadIdx.x != 0) return;
+        TileAhead& to = sm.ahead[tile % kAheadSlots];
+        if (left == 0) {
+            if (++job >= n_jobs) {
+                to.keys = 0;
+                return;
+            }
+            const CacheJob& j = sm.jobs[job];
+            const int n_prefix = (j.prefix_keys + kNarrowKeys - 1) / kNarrowKeys;
+            left = j.tile1 - j.tile0;
+            more = j.tile0 < n_prefix;
+            key0 = (more ? j.tile0 : j.tile0 - n_prefix) * kNarrowKeys;
+            end = more ? j.prefix_keys : j.own_keys[0];
+            table = a.table + (more ? 0 : j.own_table);
         }
-        keys = min(kNarrowKeys, end - key0);
-        // this thread's rows are threadIdx / PIECES + i ROWS: a quarter of the tile (16 keys, the smallest page) is COUNT / 4 of them
-        const int row = ((int)threadIdx.x / PIECES) % 16;
-        pages[0] = (int32_t)ld_l2(table + ((key0 + min(row, keys - 1)) >> a.page_shift));
-        if (a.page_shift < 6) {
-#pragma unroll
-            for (int i = 1; i < 4; ++i) pages[i] = (int32_t)ld_l2(table + ((key0 + min(16 * i + row, keys - 1)) >> a.page_shift));
-        } else {
-            pages[1] = pages[2] = pages[3] = pages[0];
-        }
+        to.head = sm.jobs[job].head, to.key0 = key0, to.keys = min(kNarrowKeys, end - key0);
+        copy16(smem_of(to.pages), table + ((key0 >> a.page_shift) & ~3), true);
+        key0 += kNarrowKeys;
+        --left;
+        if (more && key0 >= end) key0 = 0, end = sm.jobs[job].own_keys[0], table = a.table + sm.jobs[job].own_table, more = false;
     }
     __device__ __forceinline__ void fetch() {
+        const TileAhead& t = sm.ahead[fetched % kAheadSlots];
+        const int keys = t.keys;
         if (keys > 0) {
-            const int piece = threadIdx.x % PIECES, mask = (1 << a.page_shift) - 1;
+            const int piece = threadIdx.x % PIECES, mask = (1 << a.page_shift) - 1, key0 = t.key0;
             const uint32_t stage = base + (issued % kStages) * kStageBytes<D>;
-            const T* k = static_cast<const T*>(a.k) + head * a.k_head + piece * 8;
-            const T* v = static_cast<const T*>(a.v) + head * a.v_head + piece * 8;
+            const T* k = static_cast<const T*>(a.k) + t.head * a.k_head + piece * 8;
+            const T* v = static_cast<const T*>(a.v) + t.head * a.v_head + piece * 8;
+            // this thread's rows are threadIdx / PIECES + i ROWS: a quarter of the tile (16 keys, the smallest page) is COUNT / 4 of them
+            int32_t pages[4];
+            const int first = ((int)threadIdx.x / PIECES) % 16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pages[i] = t.pages[((key0 + min(16 * i + first, keys - 1)) >> a.page_shift) & 3];
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
                 const int row = (int)threadIdx.x / PIECES + i * ROWS;
@@ -140,6 +147,8 @@ struct Stream {
             }
             ++issued;
         }
+        note(fetched + AHEAD);
+        ++fetched;
         copies_commit();
     }
     __device__ __forceinline__ uint32_t next() {   // the stage of the next tile, once it is there for everybody
@@ -260,7 +269,6 @@ __device__ __forceinline__ void narrow_job(const CacheArgs& a, const CacheJob jo
                 mma<T>(o[2 * c + 1], pf, vf[2], vf[3]);
             }
         }
-        stream.look_ahead();
     }
     if (next) query.load(a, *next);
     // the warps that share rows, added up in the order of their keys
