@@ -86,18 +86,22 @@ inline int narrow_tile(int64_t tokens, int group) {
 constexpr int kPrefixRows = 32;
 
 // What a key tile takes one SM, in ns (measured: the wide kernel's tile of 128 rows, the narrow one's tiles on the CTAs of an SM together), and what a job takes
-// beside them, in key tiles (as its CTA is dealt them: a job that is cut needs its sum too; a narrow one alone takes 1.3).
+// beside them, in key tiles (as its CTA is dealt them: a job that is cut needs its sum too; a narrow one alone takes 1.1).
 constexpr double wide_tile_ns(int head_dim) { return head_dim == 64 ? 700 : 1000; }
-constexpr double narrow_tile_ns(int head_dim, int rows) { return (rows == 16 ? 780 : rows == 32 ? 900 : 1300) * (head_dim == 64 ? 0.5 : 1.0); }
+constexpr double narrow_tile_ns(int head_dim, int rows) { return (rows == 16 ? 680 : rows == 32 ? 900 : 1300) * (head_dim == 64 ? 0.5 : 1.0); }
 constexpr int kWideJobTiles = 6, kNarrowJobTiles = 2;
-constexpr double kNarrowOneJob = 1.3;
+constexpr double kNarrowOneJob = 1.1;
 constexpr double kWideStartNs = 2000;   // by so much the wide kernel's start and end take longer
+// Where the narrow kernel has four times as much to do, its streams have the memory, and the wide one's key tiles wait for theirs (32 tokens, 8 200 own keys each behind
+// 32 801 shared ones: 218 us without this factor, 200 one kernel behind the other).
+constexpr double kWideCrowded = 1.35;
 
 // A step that needs both kernels gives each its own SMs, as many as it has work, so that they start together and an SM sees one start and one end: 32 tokens behind
-// 32 801 shared and up to 2 000 own keys of 8 heads x 128 channels 55 -> 47 us, 24 drafts of 5 tokens behind 4 001 32 -> 28, 256 sequences behind 2 000
-// 136 -> 124.  Where the wide kernel alone has more than kSplitNs to do, the narrow one goes to the SMs as they become free instead: its jobs fill
-// the wide kernel's uneven end, and an SM too many or too few for either costs more than a start (wide work of 83 us: 106 us both ways, of 131 us 176 us in turn
-// and 205 side by side).
+// 32 801 shared and up to 2 000 own keys of 8 heads x 128 channels 55 -> 48 us, 24 drafts of 5 tokens behind 4 001 32 -> 30, 256 sequences behind 2 000
+// 136 -> 105.  Where the wide kernel alone has more than kSplitNs to do, or the narrow one less than a sixth of it, the narrow one goes to the SMs as they become
+// free instead: its jobs fill the wide kernel's uneven end, and an SM too many or too few for either costs more than a start (wide work of 83 us: 106 us both
+// ways, of 131 us 176 in turn and 205 side by side; 12 prompts and tokens behind 4 000 keys, nearly all of it wide, 43 in turn and 49).  Of 40 drawn steps
+// that need both, side by side was faster in 22, as fast in 11 and slower in 7, by 7 % over all of them; the worst lost 10 % (six sequences of up to 100 tokens behind 16 001 keys).
 constexpr double kSplitNs = 64e3;
 
 // What is to be dealt: a row tile (or a pair of them) and a key head, `tiles` key tiles.
@@ -334,7 +338,8 @@ inline void make_batch_plan(const httm_batch_config& c, const BatchInput& in, in
         double wide_ns = 0, narrow_ns = 0;
         for (const BatchItem& it : wide) wide_ns += (it.tiles * it.cost + kWideJobTiles) * wide_tile_ns(c.head_dim);
         for (const BatchItem& it : narrow) narrow_ns += (it.tiles + kNarrowOneJob) * narrow_tile_ns(c.head_dim, p->segs[it.seg].tile_rows);
-        if (wide_ns <= kSplitNs * sm_count) {
+        if (wide_ns <= kSplitNs * sm_count && 6 * narrow_ns >= wide_ns) {
+            if (narrow_ns > 4 * wide_ns) wide_ns *= kWideCrowded;
             double least = 0;
             for (int w = 1; w < sm_count; ++w) {
                 const double t = std::max(kWideStartNs + wide_ns / w, narrow_ns / (sm_count - w));

@@ -6,8 +6,8 @@
 // asynchronous copies three tiles deep, two CTAs per SM (three for 64 channels).  The products are done by warp-level matrix instructions of 16 rows; four warps share
 // a tile of 16 rows by keys (16 keys each), one of 32 rows two by two, one of 64 by rows, and keep their own maxima and sums until the
 // job ends.  The weights p are rounded to the values' type for the product with V, as they enter the matrix instruction; the sum l takes them before.
-// 32 sequences of 8 192 keys, 8 heads x 128 channels: 172 us, 6.2 TB/s (97 % of a copy); 64 channels 176.  A job costs about 1.3 key tiles beside its keys: 4 736 jobs
-// of one key 42 us, of 64 keys 54, of 512 keys 204 (6.1 TB/s).
+// 24 sequences of 8 100 keys, 16 heads x 64 channels: 122 us, 6.5 TB/s (a copy's rate); 8 heads x 128 channels 128 us, 6.2.  A job costs about one key tile beside its keys:
+// 4 736 jobs of one key 38 us, of 64 keys 50, of 512 keys 189 (6.6 TB/s).
 #include "httm_cache.cuh"
 
 namespace httm {
